@@ -134,7 +134,7 @@ def _quant_k(x):
     below 7 times itself."""
     b = x.float().view(*x.shape[:-1], 4, 32)
     top = b.abs().amax(-1)
-    e = ((top.view(torch.int32) + 0x200000) >> 23).sub(2).clamp_(min=27)
+    e = ((top.view(torch.int32) + 0x200000) >> 23).sub(2).clamp_(27, 252)
     e = torch.where(torch.isfinite(top), e, torch.full_like(e, 255))
     return _codes(b * torch.exp2(127.0 - e)[..., None]).view(x.shape), e.to(torch.uint8)
 
@@ -142,7 +142,7 @@ def _quant_k(x):
 def _quant_v(x):
     """Values [..., 128] -> (codes, scale [...]): a sixth of the largest, rounded up to 6 significant bits."""
     top = x.float().abs().amax(-1)
-    s = (((top / 6.0).view(torch.int32) + 0x3FFFF) & ~0x3FFFF).view(torch.float32).clamp(min=2.0 ** -100)
+    s = (((top / 6.0).view(torch.int32) + 0x3FFFF) & ~0x3FFFF).view(torch.float32).clamp(2.0 ** -100, 1.3125 * 2.0 ** 125)
     s = torch.where(torch.isfinite(top), s, torch.full_like(s, math.nan))
     return _codes(x.float() / s[..., None]), s
 
