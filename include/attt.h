@@ -155,6 +155,30 @@ attt_status attt_attention_bwd_split(const void* q, const void* k, const void* v
                                      size_t workspace_bytes, void* stream);
 
 /* --------------------------------------------------------------------------------------
+ * Forward of the adapted attention block over whole prompts, and the backward that reads what it
+ * saved. The formulas, layouts, limits and errors of attt_attention_bwd above:
+ *     O = softmax(scale Q K^T) V over the keys s <= t of the query's episode
+ * float32 scores, softmax statistics and sums; the softmax weights are rounded to bf16 once for the
+ * product with V. An infinity or a NaN in a key or value reaches the queries that see it only.
+ *
+ * attt_attention_fwd
+ *   o    device bf16 [N][heads][128] (written);  lse  device float32 [heads][N] (written)
+ * attt_attention_bwd_saved: attt_attention_bwd without its pass over the statistics
+ *   o, lse     what attt_attention_fwd wrote for the same q, k, v, offsets and scale (read)
+ *   dsum       device float32 [heads][N]: D = rowsum(dO * O) (written)
+ *   workspace  as for attt_attention_bwd_split (attt_attention_workspace_size bytes; NULL with 0
+ *              bytes: one workgroup per key block, as attt_attention_bwd)
+ * D is formed from the O given, that is from its bf16 values. */
+attt_status attt_attention_fwd(const void* q, const void* k, const void* v, const int64_t* row_offsets,
+                               int32_t num_episodes, int64_t N, int32_t heads, int32_t kv_heads,
+                               int32_t head_dim, float scale, void* o, float* lse, void* stream);
+attt_status attt_attention_bwd_saved(const void* q, const void* k, const void* v, const void* o,
+                                     const float* lse, const void* dout, const int64_t* row_offsets,
+                                     int32_t num_episodes, int64_t N, int32_t heads, int32_t kv_heads,
+                                     int32_t head_dim, float scale, void* dq, void* dk, void* dv,
+                                     float* dsum, void* workspace, size_t workspace_bytes, void* stream);
+
+/* --------------------------------------------------------------------------------------
  * Update-text repetition and the sequence-level filter (Sec. 3.2, Eq. 6-7; tau of Appendix C):
  *     rho(x_k) = max over x' in H_k of J(W(x_k), W(x')),   J(A, B) = |A & B| / |A | B|,
  *     nu(x_k) = 1 - rho(x_k),   skip the update when nu < tau   (tau = 0.5 in the paper)
@@ -440,6 +464,99 @@ typedef struct attt_lora_swap_item {
 } attt_lora_swap_item;
 
 attt_status attt_lora_hot_swap(const attt_lora_swap_item* items, int32_t count, void* stream);
+
+/* --------------------------------------------------------------------------------------
+ * Serving side: a key/value cache in 4 bits, and the attention over it. Concurrent episodes decode
+ * over long histories (Appendix A); at 134 bytes per token and key/value head instead of 512, a
+ * decoding step reads a quarter of the bytes.
+ *
+ * The cache is paged: [pages][kv_heads] records of ATTT_KV4_RECORD_BYTES, a page holding
+ * ATTT_KV4_PAGE_TOKENS tokens; row e of the page table lists the pages of sequence e in order.
+ * Codes are e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives; to nearest, ties to the even code). A record:
+ *   bytes 0      key codes [128 tokens][64], two a byte along the head dimension, low half first
+ *   bytes 8192   value codes [128 elements][64], two a byte along the tokens: position
+ *                32 a + 4 b + c (a, c < 4; b < 8) is token 16 b + 4 a + c of the page
+ *   bytes 16384  key scales [4][16][8]: byte b of the 32 elements 32 i .. of token t at [i][t % 16][t / 16],
+ *                the factor 2^(b - 127), 255: not a number
+ *   bytes 16896  value scales, bf16 [128], in the order of the value codes
+ * A key's scale is the power of two with exponent floor(log2(largest of its 32 magnitudes)) - 2, one more where
+ * the largest is 1.75 powers of two or above; a value's is a sixth of the largest of its 128
+ * magnitudes, rounded up to 6 significant bits; both at least 2^-100. What a record stands for, code
+ * times scale, is exact in bf16. Where a key's 32 elements, or a value's 128, hold an infinity or a
+ * NaN, the scale is NaN and so is all it scales.
+ *
+ * Both calls take rows of new tokens, packed: rows row_offsets[e] .. row_offsets[e+1] - 1 are the
+ * last of sequence e's lengths[e] tokens, so row i is at position lengths[e] - (rows of e) + i. A row
+ * at a negative position (an idle slot of a batch: length 0) is not stored and sees nothing.
+ *
+ * attt_kv4_append writes the rows' keys and values into their places; the rest of the pages stays.
+ * attt_kv4_attention lets every row attend to the positions up to its own (append first):
+ *     O = softmax(scale Q K^T) V,   lse = log sum exp;   a row that sees nothing: O = 0, lse = -inf
+ * float32 scores, softmax statistics and sums; the softmax weight times the value's scale is rounded
+ * to bf16 once. Bits of the cache that no token was written to are never used.
+ *
+ * cache         device [pages][kv_heads][ATTT_KV4_RECORD_BYTES] (attt_kv4_cache_size bytes)
+ * k, v          device bf16 [N][kv_heads][128];  q: device bf16 [N][heads][128]
+ * page_table    device int32 [num_sequences][table_width]: page ids in [0, pages); entries past a
+ *               sequence's length are not read. Sequences may share pages that no call appends to.
+ * lengths       device int32 [num_sequences]
+ * row_offsets   host int64 [num_sequences + 1] from 0 to N, or NULL: one row per sequence (N = num_sequences)
+ * k_held, v_held  device bf16 [N][kv_heads][128] or both NULL: the values the cache now stands for; 0
+ *               for rows that are not stored
+ * max_length    host bound of the lengths, at most 128 table_width: it decides how many workgroups share a
+ *               sequence, so a tight one is faster
+ * o, lse        device bf16 [N][heads][128], float32 [heads][N] (written)
+ * workspace     attt_kv4_attention_workspace_size bytes for the same offsets, heads and max_length
+ *               (may be 0), 256-byte aligned
+ * lengths and the table are read on the device, so a captured graph follows them. What the host
+ * cannot see is reported in the outputs: rows of a sequence with a length above max_length (append: above 128
+ * table_width), or whose table names a page outside [0, pages), are NaN (append: such rows are not
+ * stored). Nothing outside the cache is touched.
+ * Errors (before any HIP call): ATTT_EINVAL for bad offsets, null or misaligned pointers, heads not a multiple
+ * of kv_heads, a bad scale or max_length; ATTT_ENOSPACE; ATTT_EUNSUPPORTED for head_dim != 128, heads >= 2^16,
+ * N x heads >= 2^31 or a table of 2^31 tokens.
+ * ------------------------------------------------------------------------------------ */
+#define ATTT_KV4_PAGE_TOKENS 128
+#define ATTT_KV4_RECORD_BYTES 17152
+attt_status attt_kv4_cache_size(int64_t pages, int32_t kv_heads, int32_t head_dim, size_t* bytes);
+attt_status attt_kv4_append(void* cache, int64_t pages, const void* k, const void* v,
+                            const int32_t* page_table, int64_t table_width, const int32_t* lengths,
+                            const int64_t* row_offsets, int32_t num_sequences, int64_t N,
+                            int32_t kv_heads, int32_t head_dim, void* k_held, void* v_held, void* stream);
+attt_status attt_kv4_attention_workspace_size(const int64_t* row_offsets, int32_t num_sequences, int64_t N,
+                                              int32_t heads, int32_t kv_heads, int32_t head_dim,
+                                              int64_t max_length, size_t* bytes);
+attt_status attt_kv4_attention(const void* q, const void* cache, int64_t pages, const int32_t* page_table,
+                               int64_t table_width, const int32_t* lengths, const int64_t* row_offsets,
+                               int32_t num_sequences, int64_t N, int32_t heads, int32_t kv_heads,
+                               int32_t head_dim, int64_t max_length, float scale, void* o, float* lse,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
+/* --------------------------------------------------------------------------------------
+ * Log-probabilities of given tokens through the LM head (the model's own account of a text that the
+ * update of Eq. 10 trains on, or of the tokens it has just produced), with the entropy of every
+ * row's distribution and its most probable alternatives:
+ *     z_t = W h_t,  lse_t = log sum_v exp(z_tv),  logp_t = z_{t, labels[t]} - lse_t
+ *     entropy_t = -sum_v p_tv log p_tv,  p_t = softmax(z_t)
+ *     top_ids[t][k], top_logp[t][k] = v, z_tv - lse_t of the k-th largest logit; equal logits in the order of their ids
+ * Logits and all sums in float32. The gradient of logp is that of attt_weighted_ce_fwd_bwd.
+ *
+ * hidden        device [N, d] of dtype;  lm_head: device [V, d] of dtype;  labels: device int32 [N]
+ * N, d, V       N >= 0, 1 <= d < 2^20 with d % 8 == 0, 1 <= V <= 2^30
+ * dtype         ATTT_F32 or ATTT_BF16
+ * top           0 <= top <= V, at most ATTT_LOGPROBS_MAX_TOP
+ * logp          device float [N];  entropy: device float [N] or NULL
+ * top_ids, top_logp  device int32, float [N][top] (not read for top = 0)
+ * workspace     attt_logprobs_workspace_size bytes, 256-byte aligned
+ * A label outside [0, V): logp is NaN, the rest as ever. A row without a finite lse (a NaN or +inf logit, or only
+ * -inf): NaN everywhere, ids -1. Errors (before any HIP call): ATTT_EINVAL, ATTT_ENOSPACE, ATTT_EUNSUPPORTED.
+ * ------------------------------------------------------------------------------------ */
+#define ATTT_LOGPROBS_MAX_TOP 32
+attt_status attt_logprobs_workspace_size(int64_t N, int64_t d, int64_t V, int32_t dtype, int32_t top, size_t* bytes);
+attt_status attt_token_logprobs(const void* hidden, const void* lm_head, const int32_t* labels, int64_t N,
+                                int64_t d, int64_t V, int32_t dtype, int32_t top, float* logp, float* entropy,
+                                int32_t* top_ids, float* top_logp, void* workspace, size_t workspace_bytes,
+                                void* stream);
 
 /* --------------------------------------------------------------------------------------
  * Kernel timing (diagnostics). When enabled, every launch of a named kernel is bracketed

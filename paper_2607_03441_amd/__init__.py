@@ -2,8 +2,8 @@
 (arXiv 2607.03441: n-gram token weights, Eq. 8-9; weighted LM-head cross-entropy, Eq. 10;
 LoRA adapter gradients).
 
-This module only marshals arguments (those of the calls that take a list of problems natively,
-csrc/binding.cpp): torch tensors provide device memory and the current HIP stream, and every step
+This module only marshals arguments (those of the calls that take a list of problems, and of the
+serving and prompt calls, natively, csrc/binding.cpp): torch tensors provide device memory and the current HIP stream, and every step
 runs in the library's HIP kernels. There is no fallback: if the library is not built, every call
 raises.
 """
@@ -17,6 +17,8 @@ __all__ = ["load", "lib_path", "AtttError", "ngram_weights", "ngram_weights_noal
            "ngram_set_size", "ngram_set_init", "ngram_set_append", "ngram_set_weights",
            "weighted_ce_fwd_bwd", "ce_workspace_size", "ce_head_t_size", "ce_head_transpose", "lora_grad", "lora_workspace_size", "lora_sgd_step",
            "lora_forward", "lora_hot_swap",
+           "attention_fwd", "attention_bwd_saved", "kv4_cache_size", "kv4_append", "kv4_attention",
+           "kv4_attention_workspace_size", "token_logprobs", "logprobs_workspace_size",
            "timing_enable", "timing_reset", "timing_read", "kernel_names", "version",
            "F32", "BF16", "LoraProblem", "LoraParam", "LoraFwdProblem", "LoraSwapItem"]
 
@@ -91,6 +93,11 @@ def load():
     L.attt_attention_bwd_split.restype = i32
     L.attt_attention_bwd_split.argtypes = [vp, vp, vp, vp, p64, i32, i64, i32, i32, i32, f32, vp, vp, vp, vp, vp, vp,
                                            sz, vp]
+    L.attt_attention_fwd.restype = i32
+    L.attt_attention_fwd.argtypes = [vp, vp, vp, p64, i32, i64, i32, i32, i32, f32, vp, vp, vp]
+    L.attt_attention_bwd_saved.restype = i32
+    L.attt_attention_bwd_saved.argtypes = [vp, vp, vp, vp, vp, vp, p64, i32, i64, i32, i32, i32, f32, vp, vp, vp, vp, vp,
+                                           sz, vp]
     L.attt_repetition_workspace_size.restype = i32
     L.attt_repetition_workspace_size.argtypes = [p64, p64, i32, psz]
     L.attt_update_repetition.restype = i32
@@ -130,6 +137,18 @@ def load():
     L.attt_lora_forward.argtypes = [ctypes.POINTER(LoraFwdProblem), i32, vp]
     L.attt_lora_hot_swap.restype = i32
     L.attt_lora_hot_swap.argtypes = [ctypes.POINTER(LoraSwapItem), i32, vp]
+    L.attt_kv4_cache_size.restype = i32
+    L.attt_kv4_cache_size.argtypes = [i64, i32, i32, psz]
+    L.attt_kv4_append.restype = i32
+    L.attt_kv4_append.argtypes = [vp, i64, vp, vp, vp, i64, vp, p64, i32, i64, i32, i32, vp, vp, vp]
+    L.attt_kv4_attention_workspace_size.restype = i32
+    L.attt_kv4_attention_workspace_size.argtypes = [p64, i32, i64, i32, i32, i32, i64, psz]
+    L.attt_kv4_attention.restype = i32
+    L.attt_kv4_attention.argtypes = [vp, vp, i64, vp, i64, vp, p64, i32, i64, i32, i32, i32, i64, f32, vp, vp, vp, sz, vp]
+    L.attt_logprobs_workspace_size.restype = i32
+    L.attt_logprobs_workspace_size.argtypes = [i64, i64, i64, i32, i32, psz]
+    L.attt_token_logprobs.restype = i32
+    L.attt_token_logprobs.argtypes = [vp, vp, vp, i64, i64, i64, i32, i32, vp, vp, vp, vp, vp, sz, vp]
     L.attt_timing_enable.restype = i32
     L.attt_timing_enable.argtypes = [i32]
     L.attt_timing_reset.restype = i32
@@ -297,6 +316,27 @@ def attention_bwd(q, k, v, dout, row_offsets=None, scale=None, out=None, workspa
     else:
         _check(L.attt_attention_bwd(*args, _stream_ptr()))
     return dq, dk, dv, lse, dsum
+
+
+def attention_fwd(q, k, v, row_offsets=None, scale=None, out=None):
+    """Causal attention over whole prompts, packed episodes, grouped heads: (o, lse).
+
+    q: device bf16 [N, heads, 128]; k, v: [N, kv_heads, 128]; row_offsets: host int64 episode offsets
+    or None; scale defaults to 1/sqrt(128). o: bf16 [N, heads, 128], lse: float32 [heads, N], both for
+    attention_bwd_saved; out: those two, to be written into. Runs on the tensors' device, on its current stream."""
+    status, o, lse = _native().attention_fwd(q, k, v, row_offsets, scale, out)
+    _check(status)
+    return o, lse
+
+
+def attention_bwd_saved(q, k, v, o, lse, dout, row_offsets=None, scale=None, out=None, workspace=None):
+    """Backward of attention_fwd from what it returned: (dq, dk, dv, dsum).
+
+    The arguments of attention_fwd, its o and lse, and dout like q. dsum: float32 [heads, N], the row
+    sums of dout * o. workspace: as for attention_bwd."""
+    status, dq, dk, dv, dsum = _native().attention_bwd_saved(q, k, v, o, lse, dout, row_offsets, scale, out, workspace)
+    _check(status)
+    return dq, dk, dv, dsum
 
 
 def repetition_workspace_size(text_offsets, episode_texts):
@@ -541,6 +581,75 @@ def lora_hot_swap(pairs):
     """Adapter swap into serving: each (src, dst) pair, src a float32 tensor and dst a bfloat16
     tensor of equal numel, gets dst = src rounded to nearest even, all in one launch."""
     _check(_native().lora_hot_swap(pairs))
+
+
+# ------------------------------------------------------------------------------------------
+KV4_PAGE = 128       # tokens per page of the 4-bit cache
+KV4_RECORD = 17152   # bytes per page and key/value head
+
+
+def kv4_cache_size(pages, kv_heads, head_dim=128):
+    """Bytes of a cache of `pages` pages: a uint8 tensor [pages, kv_heads, KV4_RECORD]."""
+    out = ctypes.c_size_t(0)
+    _check(load().attt_kv4_cache_size(int(pages), int(kv_heads), int(head_dim), ctypes.byref(out)))
+    return out.value
+
+
+def kv4_append(cache, k, v, page_table, lengths, row_offsets=None, want_held=False, out=None):
+    """Write new tokens' keys and values into the paged 4-bit cache.
+
+    cache: device uint8 [pages, kv_heads, KV4_RECORD]; k, v: device bf16 [N, kv_heads, 128], the new rows of
+    all sequences, packed; page_table: device int32 [E, width]; lengths: device int32 [E], tokens of
+    every sequence with the new rows; row_offsets: host [E+1], or None for one row per sequence.
+    Row i of sequence e goes to position lengths[e] - (rows of e) + i; rows at negative positions are not
+    stored. Returns (k_held, v_held), the bf16 values the cache now stands for, with want_held or `out`
+    (two tensors to write them into), else None."""
+    status, kh, vh = _native().kv4_append(cache, k, v, page_table, lengths, row_offsets, want_held, out)
+    _check(status)
+    return None if kh is None else (kh, vh)
+
+
+def kv4_attention_workspace_size(N, heads, kv_heads, max_length, row_offsets=None, sequences=None, head_dim=128):
+    """Bytes of the workspace kv4_attention uses; sequences: their number where row_offsets is None (default N)."""
+    L = load()
+    if row_offsets is None:
+        E, op = N if sequences is None else sequences, None
+    else:
+        oo, op = _offsets(row_offsets)
+        E = len(oo) - 1
+    out = ctypes.c_size_t(0)
+    _check(L.attt_kv4_attention_workspace_size(op, E, N, heads, kv_heads, head_dim, int(max_length), ctypes.byref(out)))
+    return out.value
+
+
+def kv4_attention(q, cache, page_table, lengths, row_offsets=None, scale=None, max_length=None, out=None, workspace=None):
+    """Attention of new tokens over the 4-bit cache, their own keys and values appended before: (o, lse).
+
+    q: device bf16 [N, heads, 128]; cache, page_table, lengths and row_offsets as for kv4_append. A row sees
+    the positions up to its own; one that sees none has o = 0 and lse = -inf. max_length: host bound of
+    the lengths (default: the table's width); a tight one splits the work better. Sequences beyond it, or
+    with pages outside the cache, give NaN. workspace: uint8, allocated here when absent or too small."""
+    status, o, lse = _native().kv4_attention(q, cache, page_table, lengths, row_offsets, scale, max_length, out, workspace)
+    _check(status)
+    return o, lse
+
+
+def logprobs_workspace_size(N, d, V, dtype, top=0):
+    out = ctypes.c_size_t(0)
+    _check(load().attt_logprobs_workspace_size(N, d, V, dtype, top, ctypes.byref(out)))
+    return out.value
+
+
+def token_logprobs(hidden, lm_head, labels, top=0, out=None, workspace=None):
+    """Log-probabilities of given tokens through the LM head: (logp, entropy, top_ids, top_logp).
+
+    hidden: device [N, d], lm_head: [V, d] (both float32 or bfloat16), labels: int32 [N]. logp, entropy:
+    float32 [N]; top_ids (int32) and top_logp (float32) [N, top]: the `top` most probable tokens of
+    every row, equal ones in the order of their ids (None for top = 0). out: those tensors (the first two
+    for top = 0; None in the entropy's place leaves it out)."""
+    status, logp, entropy, ids, lp = _native().token_logprobs(hidden, lm_head, labels, top, out, workspace)
+    _check(status)
+    return logp, entropy, ids, lp
 
 
 # ------------------------------------------------------------------------------------------

@@ -16,8 +16,9 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libattt.so")
 BINDING = os.path.join(HERE, "_binding.so")
 
-DEVICE_SOURCES = ["ngram.hip", "ngram_set.hip", "ce.hip", "ce_fused.hip", "lora.hip", "repetition.hip", "attention.hip", "lora_serve.hip"]
-HOST_SOURCES = ["api.cpp"]
+DEVICE_SOURCES = ["ngram.hip", "ngram_set.hip", "ce.hip", "ce_fused.hip", "lora.hip", "repetition.hip", "attention.hip", "attention_fwd.hip",
+                  "lora_serve.hip", "kv4.hip", "logprobs.hip"]
+HOST_SOURCES = ["api.cpp", "api_serving.cpp"]
 ARCH = "gfx950"
 
 

@@ -8,11 +8,13 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
 #include <string>
 #include <type_traits>
 #include <vector>
 
+#include "api_util.hpp"
 #include "attt.h"
 #include "internal.hpp"
 
@@ -26,8 +28,7 @@ static_assert(kNgramScratchBytes == ATTT_NGRAM_NOALLOC_SCRATCH_BYTES, "header an
 // ------------------------------------------------------------------------------------------
 static thread_local std::string g_last_error;
 
-static attt_status fail(attt_status code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
-static attt_status fail(attt_status code, const char* fmt, ...) {
+attt_status attt::fail(attt_status code, const char* fmt, ...) {
   char buf[512];
   va_list ap;
   va_start(ap, fmt);
@@ -37,23 +38,14 @@ static attt_status fail(attt_status code, const char* fmt, ...) {
   return code;
 }
 
-static attt_status hip_fail(hipError_t e, const char* where) {
-  return fail(ATTT_EHIP, "%s: %s", where, hipGetErrorString(e));
-}
-
-#define HIP_TRY(expr, where)                  \
-  do {                                        \
-    hipError_t e_ = (expr);                   \
-    if (e_ != hipSuccess) return hip_fail(e_, where); \
-  } while (0)
-
 namespace attt {
 
 static const char* kKernelNames[K_NUM_KERNELS] = {
     "ngram_count", "ngram_weight", "ngram_table", "ce_fwd_lse", "ce_label_logit", "ce_row_reduce",
     "ce_loss", "ce_head_transpose", "ce_bwd_dz", "ce_bwd_dh", "ce_overflow_guard", "lora_u_du", "lora_dadb",
     "lora_reduce", "ngram_set", "ngram_set_weight", "lora_sgd", "ce_fused_bwd", "rep_count", "rep_reduce", "attn_fwd_stats",
-    "attn_dkdv", "attn_dq", "lora_fwd", "lora_swap"};
+    "attn_dkdv", "attn_dq", "lora_fwd", "lora_swap", "attn_fwd", "attn_dsum", "kv4_append", "kv4_attention", "kv4_join",
+    "logprob_logits", "logprob_rows", "logprob_join"};
 
 const char* kernel_name(int id) { return (id >= 0 && id < K_NUM_KERNELS) ? kKernelNames[id] : nullptr; }
 
@@ -144,27 +136,6 @@ attt_status attt_timing_read(const char* kernel, double* total_ms, int64_t* laun
 const char* attt_timing_kernel_name(int32_t i) { return kernel_name(i); }
 
 }  // extern "C"
-
-// ------------------------------------------------------------------------------------------
-// Helpers
-// ------------------------------------------------------------------------------------------
-static inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
-static inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-static inline int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
-static inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-static inline bool aligned256(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 255u) == 0; }
-
-static attt_status check_offsets(const char* what, const int64_t* off, int32_t E, int64_t limit) {
-  if (!off) return fail(ATTT_EINVAL, "%s: offsets pointer is null", what);
-  if (off[0] != 0) return fail(ATTT_EINVAL, "%s: offsets[0] must be 0", what);
-  for (int32_t e = 0; e < E; ++e) {
-    if (off[e + 1] < off[e]) return fail(ATTT_EINVAL, "%s: offsets decrease at episode %d", what, e);
-    if (off[e + 1] - off[e] > limit)
-      return fail(ATTT_EUNSUPPORTED, "%s: episode %d holds %lld entries (limit %lld)", what, e,
-                  (long long)(off[e + 1] - off[e]), (long long)limit);
-  }
-  return ATTT_OK;
-}
 
 // ------------------------------------------------------------------------------------------
 // n-gram exposure and weights
@@ -523,21 +494,38 @@ attt_status attn_check(const int64_t*& off, int64_t (&single)[2], int32_t num_ep
   return ATTT_OK;
 }
 
-attt_status attn_run(const void* q, const void* k, const void* v, const void* dout, const int64_t* row_offsets,
-                     int32_t num_episodes, int64_t N, int32_t heads, int32_t kv_heads, int32_t head_dim, float scale,
-                     void* dq, void* dk, void* dv, float* lse, float* dsum, bool split, void* workspace,
-                     size_t workspace_bytes, void* stream) {
+attt_status attn_pointers(std::initializer_list<const void*> ptrs) {
+  for (const void* ptr : ptrs) {
+    if (!ptr) return fail(ATTT_EINVAL, "attention: null pointer");
+    if (!aligned16(ptr)) return fail(ATTT_EINVAL, "attention: device pointers must be 16-byte aligned");
+  }
+  return ATTT_OK;
+}
+
+// Episodes e0 .. of at most a launch.
+AttnBatch attn_batch(const int64_t* off, int32_t e0, int32_t num_episodes) {
+  AttnBatch b{};
+  b.count = std::min<int32_t>(kEpBatch, num_episodes - e0);
+  for (int i = 0; i < b.count; ++i) {
+    b.e[i].row0 = off[e0 + i];
+    b.e[i].L = (int32_t)(off[e0 + i + 1] - off[e0 + i]);
+  }
+  return b;
+}
+
+// o, where given: the forward's output, whose statistics then are not computed again (lse is read, not written).
+attt_status attn_run(const void* q, const void* k, const void* v, const void* o, const void* dout,
+                     const int64_t* row_offsets, int32_t num_episodes, int64_t N, int32_t heads, int32_t kv_heads,
+                     int32_t head_dim, float scale, void* dq, void* dk, void* dv, float* lse, float* dsum, bool split,
+                     void* workspace, size_t workspace_bytes, void* stream) {
   int64_t single[2];
   const int64_t* off = row_offsets;
   attt_status st = attn_check(off, single, num_episodes, N, heads, kv_heads, head_dim);
   if (st) return st;
   if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(ATTT_EINVAL, "attention: scale must be finite and > 0");
   if (N == 0) return ATTT_OK;
-  const void* ptrs[] = {q, k, v, dout, dq, dk, dv, lse, dsum};
-  for (const void* ptr : ptrs) {
-    if (!ptr) return fail(ATTT_EINVAL, "attention: null pointer");
-    if (!aligned16(ptr)) return fail(ATTT_EINVAL, "attention: device pointers must be 16-byte aligned");
-  }
+  st = attn_pointers({q, k, v, o ? o : q, dout, dq, dk, dv, lse, dsum});
+  if (st) return st;
   std::vector<AttnSplit> splits;
   for (int32_t e0 = 0; e0 < num_episodes; e0 += kEpBatch) {
     const AttnSplit sp = attn_split(off + e0, std::min<int32_t>(kEpBatch, num_episodes - e0), heads, kv_heads, split);
@@ -552,6 +540,7 @@ attt_status attn_run(const void* q, const void* k, const void* v, const void* do
   a.k = static_cast<const bf16_t*>(k);
   a.v = static_cast<const bf16_t*>(v);
   a.dout = static_cast<const bf16_t*>(dout);
+  a.o = const_cast<bf16_t*>(static_cast<const bf16_t*>(o));
   a.dq = static_cast<bf16_t*>(dq);
   a.dk = static_cast<bf16_t*>(dk);
   a.dv = static_cast<bf16_t*>(dv);
@@ -562,18 +551,14 @@ attt_status attn_run(const void* q, const void* k, const void* v, const void* do
   a.kv_heads = kv_heads;
   a.scale = scale;
   hipStream_t s = static_cast<hipStream_t>(stream);
+  if (o) HIP_TRY(launch_attn_dsum(a, s), "attn_dsum");
   for (int32_t e0 = 0; e0 < num_episodes; e0 += kEpBatch) {
-    AttnBatch b{};
-    b.count = std::min<int32_t>(kEpBatch, num_episodes - e0);
-    for (int i = 0; i < b.count; ++i) {
-      b.e[i].row0 = off[e0 + i];
-      b.e[i].L = (int32_t)(off[e0 + i + 1] - off[e0 + i]);
-    }
+    AttnBatch b = attn_batch(off, e0, num_episodes);
     b.tiles = splits[e0 / kEpBatch].tiles;
     b.splits = splits[e0 / kEpBatch].splits;
     b.chunk = splits[e0 / kEpBatch].chunk;
     b.part = static_cast<float*>(workspace);
-    for (int kernel = 0; kernel < 3; ++kernel)
+    for (int kernel = o ? 1 : 0; kernel < 3; ++kernel)
       HIP_TRY(launch_attn(kernel, a, b, s), kernel == 0 ? "attn_fwd_stats" : kernel == 1 ? "attn_dkdv" : "attn_dq");
   }
   return ATTT_OK;
@@ -598,7 +583,7 @@ extern "C" attt_status attt_attention_bwd(const void* q, const void* k, const vo
                                           const int64_t* row_offsets, int32_t num_episodes, int64_t N,
                                           int32_t heads, int32_t kv_heads, int32_t head_dim, float scale,
                                           void* dq, void* dk, void* dv, float* lse, float* dsum, void* stream) {
-  return attn_run(q, k, v, dout, row_offsets, num_episodes, N, heads, kv_heads, head_dim, scale, dq, dk, dv, lse, dsum,
+  return attn_run(q, k, v, nullptr, dout, row_offsets, num_episodes, N, heads, kv_heads, head_dim, scale, dq, dk, dv, lse, dsum,
                   false, nullptr, 0, stream);
 }
 
@@ -607,8 +592,44 @@ extern "C" attt_status attt_attention_bwd_split(const void* q, const void* k, co
                                                 int32_t heads, int32_t kv_heads, int32_t head_dim, float scale,
                                                 void* dq, void* dk, void* dv, float* lse, float* dsum, void* workspace,
                                                 size_t workspace_bytes, void* stream) {
-  return attn_run(q, k, v, dout, row_offsets, num_episodes, N, heads, kv_heads, head_dim, scale, dq, dk, dv, lse, dsum,
+  return attn_run(q, k, v, nullptr, dout, row_offsets, num_episodes, N, heads, kv_heads, head_dim, scale, dq, dk, dv, lse, dsum,
                   true, workspace, workspace_bytes, stream);
+}
+
+extern "C" attt_status attt_attention_fwd(const void* q, const void* k, const void* v, const int64_t* row_offsets,
+                                          int32_t num_episodes, int64_t N, int32_t heads, int32_t kv_heads,
+                                          int32_t head_dim, float scale, void* o, float* lse, void* stream) {
+  int64_t single[2];
+  const int64_t* off = row_offsets;
+  attt_status st = attn_check(off, single, num_episodes, N, heads, kv_heads, head_dim);
+  if (st) return st;
+  if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(ATTT_EINVAL, "attention: scale must be finite and > 0");
+  if (N == 0) return ATTT_OK;
+  st = attn_pointers({q, k, v, o, lse});
+  if (st) return st;
+  AttnArgs a{};
+  a.q = static_cast<const bf16_t*>(q);
+  a.k = static_cast<const bf16_t*>(k);
+  a.v = static_cast<const bf16_t*>(v);
+  a.o = static_cast<bf16_t*>(o);
+  a.lse = lse;
+  a.N = (int32_t)N;
+  a.heads = heads;
+  a.kv_heads = kv_heads;
+  a.scale = scale;
+  for (int32_t e0 = 0; e0 < num_episodes; e0 += kEpBatch)
+    HIP_TRY(launch_attn_fwd(a, attn_batch(off, e0, num_episodes), static_cast<hipStream_t>(stream)), "attn_fwd");
+  return ATTT_OK;
+}
+
+extern "C" attt_status attt_attention_bwd_saved(const void* q, const void* k, const void* v, const void* o,
+                                                const float* lse, const void* dout, const int64_t* row_offsets,
+                                                int32_t num_episodes, int64_t N, int32_t heads, int32_t kv_heads,
+                                                int32_t head_dim, float scale, void* dq, void* dk, void* dv,
+                                                float* dsum, void* workspace, size_t workspace_bytes, void* stream) {
+  if (N > 0 && !o) return fail(ATTT_EINVAL, "attention: null pointer");
+  return attn_run(q, k, v, o, dout, row_offsets, num_episodes, N, heads, kv_heads, head_dim, scale, dq, dk, dv,
+                  const_cast<float*>(lse), dsum, workspace != nullptr, workspace, workspace_bytes, stream);
 }
 
 // ------------------------------------------------------------------------------------------

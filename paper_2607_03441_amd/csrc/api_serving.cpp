@@ -1,0 +1,312 @@
+// C ABI of the serving operators beside the LoRA forward: the 4-bit key/value cache with its attention, and the
+// log-probabilities of given tokens. As in api.cpp: validation on the host before any HIP call, planning, launches on
+// the caller's stream.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <initializer_list>
+
+#include "api_util.hpp"
+#include "attt.h"
+#include "internal.hpp"
+
+using namespace attt;
+
+static_assert(kKv4Page == ATTT_KV4_PAGE_TOKENS && kKv4Record == ATTT_KV4_RECORD_BYTES, "header and library agree");
+static_assert(kLpMaxTop == ATTT_LOGPROBS_MAX_TOP, "header and library agree");
+
+namespace {
+
+// ------------------------------------------------------------------------------------------
+// 4-bit key/value cache
+// ------------------------------------------------------------------------------------------
+attt_status kv4_heads(int32_t kv_heads, int32_t head_dim) {
+  if (head_dim != 128) return fail(ATTT_EUNSUPPORTED, "kv4: head_dim must be 128 (got %d)", head_dim);
+  if (kv_heads < 1) return fail(ATTT_EINVAL, "kv4: kv_heads must be >= 1 (got %d)", kv_heads);
+  if (kv_heads >= (1 << 16)) return fail(ATTT_EUNSUPPORTED, "kv4: kv_heads must be < 2^16 (got %d)", kv_heads);
+  return ATTT_OK;
+}
+
+attt_status kv4_pointers(std::initializer_list<const void*> ptrs) {
+  for (const void* p : ptrs) {
+    if (!p) return fail(ATTT_EINVAL, "kv4: null pointer");
+    if (!aligned16(p)) return fail(ATTT_EINVAL, "kv4: device pointers must be 16-byte aligned");
+  }
+  return ATTT_OK;
+}
+
+// Rows of each sequence: given offsets, or one row each.
+struct Rows {
+  const int64_t* off;
+  int64_t begin(int32_t e) const { return off ? off[e] : e; }
+  int64_t count(int32_t e) const { return off ? off[e + 1] - off[e] : 1; }
+};
+
+attt_status kv4_check(const Rows& rows, int32_t E, int64_t N, int32_t heads) {
+  if (E < 1) return fail(ATTT_EINVAL, "kv4: num_sequences must be >= 1 (got %d)", E);
+  if (N < 0) return fail(ATTT_EINVAL, "kv4: N must be >= 0");
+  if (N * heads >= INT32_MAX) return fail(ATTT_EUNSUPPORTED, "kv4: N x heads must be < 2^31");
+  if (rows.off) {
+    attt_status st = check_offsets("kv4 rows", rows.off, E, INT32_MAX);
+    if (st) return st;
+  }
+  if (rows.begin(E) != N)
+    return fail(ATTT_EINVAL, "kv4: rows of %d sequences end at %lld, not at N = %lld", E, (long long)rows.begin(E), (long long)N);
+  return ATTT_OK;
+}
+
+attt_status kv4_table(const int32_t* table, int64_t width, const int32_t* lengths, int64_t pages) {
+  if (pages < 0) return fail(ATTT_EINVAL, "kv4: pages must be >= 0");
+  if (pages > INT32_MAX) return fail(ATTT_EUNSUPPORTED, "kv4: more than 2^31 - 1 pages");
+  if (width < 1) return fail(ATTT_EINVAL, "kv4: table_width must be >= 1 (got %lld)", (long long)width);
+  if (width > INT32_MAX / kKv4Page) return fail(ATTT_EUNSUPPORTED, "kv4: table_width %lld passes 2^31 - 1 tokens", (long long)width);
+  if (!table || !lengths) return fail(ATTT_EINVAL, "kv4: null pointer");
+  return ATTT_OK;
+}
+
+// The attention's launch: tiles of 16 query rows per workgroup, and how many pages a split of a sequence has.
+// A tile costs a workgroup 64 registers per lane and its own products, while every tile reads the page again where
+// the rows are cut into more workgroups.
+struct Kv4Plan {
+  int32_t row_tiles = 1, chunk = 1, splits = 1;
+  int64_t units = 0;
+  size_t bytes() const {
+    return splits > 1 ? (size_t)units * splits * 16 * row_tiles * (128 * sizeof(float) + sizeof(float2)) : 0;
+  }
+};
+
+Kv4Plan kv4_plan(const Rows& rows, int32_t E, int32_t heads, int32_t kv_heads, int64_t max_length) {
+  Kv4Plan P;
+  const int64_t g = heads / kv_heads;
+  int64_t most = 0;
+  for (int32_t e = 0; e < E; ++e) most = std::max(most, rows.count(e) * g);
+  P.row_tiles = most <= 16 ? 1 : most <= 32 ? 2 : 4;
+  for (int32_t e = 0; e < E; ++e) P.units += ceil_div(rows.count(e) * g, 16 * P.row_tiles) * kv_heads;
+  const int64_t pages = std::max<int64_t>(1, ceil_div(max_length, kKv4Page));
+  // four waves take a split's pages in turn; about four workgroups per CU
+  const int64_t chunk = std::max<int64_t>(4, round_up(ceil_div(pages * P.units, 1024), 4));
+  P.chunk = (int32_t)std::min(chunk, round_up(pages, 4));
+  P.splits = (int32_t)ceil_div(pages, P.chunk);
+  return P;
+}
+
+// Sequences e0 .. of at most a launch; `blk0`: row blocks before them.
+Kv4Batch kv4_batch(const Rows& rows, int32_t e0, int32_t E, int64_t group, int32_t block_rows, int64_t& blk0) {
+  Kv4Batch b{};
+  b.count = std::min<int32_t>(kEpBatch, E - e0);
+  for (int i = 0; i < b.count; ++i) {
+    b.s[i].row0 = rows.begin(e0 + i);
+    b.s[i].n = (int32_t)rows.count(e0 + i);
+    b.s[i].seq = e0 + i;
+    b.s[i].blk0 = (int32_t)blk0;
+    blk0 += ceil_div(rows.count(e0 + i) * group, block_rows);
+  }
+  return b;
+}
+
+}  // namespace
+
+extern "C" attt_status attt_kv4_cache_size(int64_t pages, int32_t kv_heads, int32_t head_dim, size_t* bytes) {
+  if (!bytes) return fail(ATTT_EINVAL, "kv4: bytes is null");
+  attt_status st = kv4_heads(kv_heads, head_dim);
+  if (st) return st;
+  if (pages < 0) return fail(ATTT_EINVAL, "kv4: pages must be >= 0");
+  if (pages > INT32_MAX) return fail(ATTT_EUNSUPPORTED, "kv4: more than 2^31 - 1 pages");
+  *bytes = (size_t)pages * kv_heads * kKv4Record;
+  return ATTT_OK;
+}
+
+extern "C" attt_status attt_kv4_append(void* cache, int64_t pages, const void* k, const void* v, const int32_t* page_table,
+                                       int64_t table_width, const int32_t* lengths, const int64_t* row_offsets,
+                                       int32_t num_sequences, int64_t N, int32_t kv_heads, int32_t head_dim, void* k_held,
+                                       void* v_held, void* stream) {
+  attt_status st = kv4_heads(kv_heads, head_dim);
+  if (st) return st;
+  const Rows rows{row_offsets};
+  st = kv4_check(rows, num_sequences, N, kv_heads);
+  if (st) return st;
+  st = kv4_table(page_table, table_width, lengths, pages);
+  if (st) return st;
+  if (!k_held != !v_held) return fail(ATTT_EINVAL, "kv4: k_held and v_held go together");
+  if (N == 0) return ATTT_OK;
+  st = k_held ? kv4_pointers({cache, k, v, k_held, v_held}) : kv4_pointers({cache, k, v});
+  if (st) return st;
+  Kv4Args a{};
+  a.cache = static_cast<uint8_t*>(cache);
+  a.pages = pages;
+  a.k = static_cast<const bf16_t*>(k);
+  a.v = static_cast<const bf16_t*>(v);
+  a.k_held = static_cast<bf16_t*>(k_held);
+  a.v_held = static_cast<bf16_t*>(v_held);
+  a.table = page_table;
+  a.width = table_width;
+  a.lengths = lengths;
+  a.N = N;
+  a.kv_heads = kv_heads;
+  int64_t blk0 = 0;
+  for (int32_t e0 = 0; e0 < num_sequences; e0 += kEpBatch)
+    HIP_TRY(launch_kv4_append(a, kv4_batch(rows, e0, num_sequences, 1, 1, blk0), static_cast<hipStream_t>(stream)), "kv4_append");
+  return ATTT_OK;
+}
+
+namespace {
+attt_status kv4_attention_check(const Rows& rows, int32_t E, int64_t N, int32_t heads, int32_t kv_heads, int32_t head_dim,
+                                int64_t max_length) {
+  attt_status st = kv4_heads(kv_heads, head_dim);
+  if (st) return st;
+  if (heads < 1 || heads % kv_heads != 0)
+    return fail(ATTT_EINVAL, "kv4: heads (%d) must be a positive multiple of kv_heads (%d)", heads, kv_heads);
+  if (heads >= (1 << 16)) return fail(ATTT_EUNSUPPORTED, "kv4: heads must be < 2^16 (got %d)", heads);
+  if (max_length < 0) return fail(ATTT_EINVAL, "kv4: max_length must be >= 0");
+  if (max_length > INT32_MAX) return fail(ATTT_EUNSUPPORTED, "kv4: max_length must be < 2^31");
+  return kv4_check(rows, E, N, heads);
+}
+}  // namespace
+
+extern "C" attt_status attt_kv4_attention_workspace_size(const int64_t* row_offsets, int32_t num_sequences, int64_t N,
+                                                         int32_t heads, int32_t kv_heads, int32_t head_dim,
+                                                         int64_t max_length, size_t* bytes) {
+  if (!bytes) return fail(ATTT_EINVAL, "kv4: bytes is null");
+  const Rows rows{row_offsets};
+  attt_status st = kv4_attention_check(rows, num_sequences, N, heads, kv_heads, head_dim, max_length);
+  if (st) return st;
+  *bytes = kv4_plan(rows, num_sequences, heads, kv_heads, max_length).bytes();
+  return ATTT_OK;
+}
+
+extern "C" attt_status attt_kv4_attention(const void* q, const void* cache, int64_t pages, const int32_t* page_table,
+                                          int64_t table_width, const int32_t* lengths, const int64_t* row_offsets,
+                                          int32_t num_sequences, int64_t N, int32_t heads, int32_t kv_heads,
+                                          int32_t head_dim, int64_t max_length, float scale, void* o, float* lse,
+                                          void* workspace, size_t workspace_bytes, void* stream) {
+  const Rows rows{row_offsets};
+  attt_status st = kv4_attention_check(rows, num_sequences, N, heads, kv_heads, head_dim, max_length);
+  if (st) return st;
+  st = kv4_table(page_table, table_width, lengths, pages);
+  if (st) return st;
+  if (max_length > table_width * kKv4Page)
+    return fail(ATTT_EINVAL, "kv4: max_length %lld passes the table's %lld pages", (long long)max_length, (long long)table_width);
+  if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(ATTT_EINVAL, "kv4: scale must be finite and > 0");
+  if (N == 0) return ATTT_OK;
+  st = kv4_pointers({q, cache, o, lse});
+  if (st) return st;
+  const Kv4Plan P = kv4_plan(rows, num_sequences, heads, kv_heads, max_length);
+  if (workspace_bytes < P.bytes()) return fail(ATTT_ENOSPACE, "kv4: workspace %zu bytes, need %zu", workspace_bytes, P.bytes());
+  if (P.bytes() && !workspace) return fail(ATTT_EINVAL, "kv4: workspace is null");
+  if (P.bytes() && !aligned256(workspace)) return fail(ATTT_EINVAL, "kv4: workspace must be 256-byte aligned");
+  Kv4Args a{};
+  a.q = static_cast<const bf16_t*>(q);
+  a.cache = const_cast<uint8_t*>(static_cast<const uint8_t*>(cache));
+  a.pages = pages;
+  a.table = page_table;
+  a.width = table_width;
+  a.lengths = lengths;
+  a.o = static_cast<bf16_t*>(o);
+  a.lse = lse;
+  a.max_length = max_length;
+  a.N = N;
+  a.heads = heads;
+  a.kv_heads = kv_heads;
+  a.chunk = P.chunk;
+  a.splits = P.splits;
+  a.scale = scale;
+  const int64_t rows_part = P.units * P.splits * 16 * P.row_tiles;
+  a.part = static_cast<float*>(workspace);
+  a.part_ml = P.splits > 1 ? reinterpret_cast<float2*>(a.part + rows_part * 128) : nullptr;
+  int64_t blk0 = 0;
+  for (int32_t e0 = 0; e0 < num_sequences; e0 += kEpBatch) {
+    const Kv4Batch b = kv4_batch(rows, e0, num_sequences, heads / kv_heads, 16 * P.row_tiles, blk0);
+    HIP_TRY(launch_kv4_attention(P.row_tiles, a, b, static_cast<hipStream_t>(stream)), "kv4_attention");
+  }
+  return ATTT_OK;
+}
+
+// ------------------------------------------------------------------------------------------
+// Log-probabilities of given tokens
+// ------------------------------------------------------------------------------------------
+namespace {
+
+struct LpPlan {
+  int64_t ldz = 0, rows = 0;  // staged logits: row length, rows at a time
+  int32_t splits = 0;
+  size_t off_stats = 0, off_lists = 0, total = 0;
+};
+
+attt_status lp_check(int64_t N, int64_t d, int64_t V, int32_t dtype, int32_t top) {
+  if (dtype != ATTT_F32 && dtype != ATTT_BF16) return fail(ATTT_EINVAL, "logprobs: unknown dtype %d", dtype);
+  if (N < 0) return fail(ATTT_EINVAL, "logprobs: N must be >= 0 (got %lld)", (long long)N);
+  if (d < 1 || d % 8 != 0) return fail(ATTT_EINVAL, "logprobs: d must be a positive multiple of 8 (got %lld)", (long long)d);
+  if (V < 1) return fail(ATTT_EINVAL, "logprobs: V must be >= 1 (got %lld)", (long long)V);
+  if (top < 0 || top > V) return fail(ATTT_EINVAL, "logprobs: top must be in [0, V] (got %d)", top);
+  if (top > ATTT_LOGPROBS_MAX_TOP) return fail(ATTT_EUNSUPPORTED, "logprobs: top must be at most %d (got %d)", ATTT_LOGPROBS_MAX_TOP, top);
+  if (N >= ((int64_t)1 << 31) || V > ((int64_t)1 << 30) || d >= ((int64_t)1 << 20))
+    return fail(ATTT_EUNSUPPORTED, "logprobs: dimensions beyond this build's limits");
+  return ATTT_OK;
+}
+
+LpPlan lp_plan(int64_t N, int64_t V, int32_t top) {
+  LpPlan P;
+  P.ldz = round_up(V, 64);
+  // rows of about 256 MiB of logits at a time
+  const int64_t fit = ((int64_t)256 << 20) / (P.ldz * 4);
+  P.rows = std::min<int64_t>(std::max<int64_t>(N, 1), fit >= 128 ? fit / 128 * 128 : std::max<int64_t>(1, fit));
+  P.splits = (int32_t)ceil_div(V, kLpRowChunk);
+  P.off_stats = align256((size_t)P.rows * P.ldz * 4);
+  P.off_lists = P.off_stats + align256((size_t)P.rows * P.splits * sizeof(float4));
+  P.total = P.off_lists + align256((size_t)P.rows * P.splits * top * sizeof(float2));
+  return P;
+}
+
+}  // namespace
+
+extern "C" attt_status attt_logprobs_workspace_size(int64_t N, int64_t d, int64_t V, int32_t dtype, int32_t top, size_t* bytes) {
+  if (!bytes) return fail(ATTT_EINVAL, "logprobs: bytes is null");
+  attt_status st = lp_check(N, d, V, dtype, top);
+  if (st) return st;
+  *bytes = lp_plan(N, V, top).total;
+  return ATTT_OK;
+}
+
+extern "C" attt_status attt_token_logprobs(const void* hidden, const void* lm_head, const int32_t* labels, int64_t N, int64_t d,
+                                           int64_t V, int32_t dtype, int32_t top, float* logp, float* entropy,
+                                           int32_t* top_ids, float* top_logp, void* workspace, size_t workspace_bytes,
+                                           void* stream) {
+  attt_status st = lp_check(N, d, V, dtype, top);
+  if (st) return st;
+  if (N == 0) return ATTT_OK;
+  if (!hidden || !lm_head || !labels || !logp) return fail(ATTT_EINVAL, "logprobs: null pointer");
+  if (top > 0 && (!top_ids || !top_logp)) return fail(ATTT_EINVAL, "logprobs: null pointer");
+  if (!aligned16(hidden) || !aligned16(lm_head))
+    return fail(ATTT_EINVAL, "logprobs: hidden and lm_head must be 16-byte aligned");
+  const LpPlan P = lp_plan(N, V, top);
+  if (workspace_bytes < P.total) return fail(ATTT_ENOSPACE, "logprobs: workspace %zu bytes, need %zu", workspace_bytes, P.total);
+  if (!workspace) return fail(ATTT_EINVAL, "logprobs: workspace is null");
+  if (!aligned256(workspace)) return fail(ATTT_EINVAL, "logprobs: workspace must be 256-byte aligned");
+  LpArgs a{};
+  a.h = hidden;
+  a.W = lm_head;
+  a.labels = labels;
+  a.logits = static_cast<float*>(workspace);
+  a.stats = reinterpret_cast<float4*>(static_cast<uint8_t*>(workspace) + P.off_stats);
+  a.lists = reinterpret_cast<float2*>(static_cast<uint8_t*>(workspace) + P.off_lists);
+  a.logp = logp;
+  a.entropy = entropy;
+  a.top_ids = top_ids;
+  a.top_logp = top_logp;
+  a.ldz = P.ldz;
+  a.N = (int32_t)N;
+  a.d = (int32_t)d;
+  a.V = (int32_t)V;
+  a.top = top;
+  a.splits = P.splits;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  for (int64_t r0 = 0; r0 < N; r0 += P.rows) {
+    a.row0 = (int32_t)r0;
+    a.rows = (int32_t)std::min(P.rows, N - r0);
+    HIP_TRY(launch_lp_logits(dtype, a, s), "logprob_logits");
+    HIP_TRY(launch_lp_rows(a, s), "logprob_rows");
+    HIP_TRY(launch_lp_join(a, s), "logprob_join");
+  }
+  return ATTT_OK;
+}

@@ -36,6 +36,14 @@ enum KernelId {
   K_ATTN_DQ,
   K_LORA_FWD,
   K_LORA_SWAP,
+  K_ATTN_PROMPT,
+  K_ATTN_DSUM,
+  K_KV4_APPEND,
+  K_KV4_ATTN,
+  K_KV4_JOIN,
+  K_LP_LOGITS,
+  K_LP_ROWS,
+  K_LP_JOIN,
   K_NUM_KERNELS
 };
 
@@ -152,6 +160,7 @@ struct AttnArgs {
   const bf16_t* k;     // [N][kv_heads][128]
   const bf16_t* v;
   const bf16_t* dout;  // [N][heads][128]
+  bf16_t* o;           // [N][heads][128]: written by the forward, read for D by the backward that is given it
   bf16_t* dq;
   bf16_t* dk;
   bf16_t* dv;
@@ -180,6 +189,68 @@ struct AttnBatch {
 };
 // kernel 0: forward statistics, 1: dK and dV, 2: dQ
 hipError_t launch_attn(int kernel, const AttnArgs& a, const AttnBatch& b, hipStream_t s);
+hipError_t launch_attn_fwd(const AttnArgs& a, const AttnBatch& b, hipStream_t s);
+hipError_t launch_attn_dsum(const AttnArgs& a, hipStream_t s);  // of all N rows
+
+// ---- serving: the 4-bit key/value cache ------------------------------------------------------------
+constexpr int kKv4Page = 128;      // tokens per page
+constexpr int kKv4Record = 17152;  // bytes of one (page, key/value head): 134 per token
+struct Kv4Args {
+  const bf16_t* q;         // [N][heads][128]
+  const bf16_t* k;         // append: [N][kv_heads][128]
+  const bf16_t* v;
+  bf16_t* k_held;          // append: what the cache then stands for, or null
+  bf16_t* v_held;
+  uint8_t* cache;          // [pages][kv_heads][kKv4Record]
+  const int32_t* table;    // [sequences][width] page ids
+  const int32_t* lengths;  // [sequences] tokens, the call's rows among them
+  bf16_t* o;               // [N][heads][128]
+  float* lse;              // [heads][N]
+  float* part;             // splits > 1: [unit][split][row][128], unit = (row block, key/value head)
+  float2* part_ml;         // [unit][split][row] maximum (base 2) and sum
+  int64_t pages, width, max_length, N;
+  int32_t heads, kv_heads;
+  int32_t chunk, splits;   // pages per split, splits of the longest sequence
+  float scale;
+};
+struct Kv4Seq {
+  int64_t row0;       // first row of the sequence
+  int32_t n;          // rows
+  int32_t seq;        // index in table and lengths
+  int32_t wg_begin;   // first workgroup (set at launch)
+  int32_t blk0;       // its first block of 16 row_tiles rows, over all sequences of the call
+};
+struct Kv4Batch {
+  int32_t count;
+  int32_t pad;
+  Kv4Seq s[kEpBatch];
+};
+hipError_t launch_kv4_append(const Kv4Args& a, Kv4Batch b, hipStream_t s);
+// row_tiles (1, 2 or 4): tiles of 16 query rows of a key/value head's group per workgroup
+hipError_t launch_kv4_attention(int row_tiles, const Kv4Args& a, const Kv4Batch& b, hipStream_t s);
+
+// ---- log-probabilities of given tokens -------------------------------------------------------------
+constexpr int kLpMaxTop = 32;       // most alternatives
+constexpr int kLpRowChunk = 4096;   // logits a workgroup of the row kernel takes
+struct LpArgs {
+  const void* h;         // [N][d]
+  const void* W;         // [V][d]
+  const int32_t* labels; // [N]
+  float* logits;         // staged rows [rows][ldz]
+  float4* stats;         // [row][split]: maximum m, sum exp(z - m), sum (z - m) exp(z - m), label logit (NaN: not here)
+  float2* lists;         // [row][split][top]: logit, id (as bits; -1: none)
+  float* logp;           // [N]
+  float* entropy;        // [N] or null
+  int32_t* top_ids;      // [N][top]
+  float* top_logp;       // [N][top]
+  int64_t ldz;
+  int32_t N, d, V, top;
+  int32_t row0, rows;    // the staged rows
+  int32_t splits;
+};
+hipError_t launch_lp_logits(int dtype, const LpArgs& a, hipStream_t s);
+hipError_t launch_lp_rows(const LpArgs& a, hipStream_t s);
+hipError_t launch_lp_join(const LpArgs& a, hipStream_t s);
 
 // ---- persistent n-gram set ---------------------------------------------------------------
 struct NgramSetJob {

@@ -1,0 +1,463 @@
+// Serving: a key/value cache in 4 bits and the attention over it, for concurrent episodes that decode over
+// long histories (Appendix A).
+//
+// The cache is paged: per page of 128 tokens and key/value head one record of kKv4Record bytes, laid out for the
+// reads of the attention kernel, whose lane (l16, q4) of a wave takes in every load 16 bytes that it
+// multiplies itself:
+//   keys    e2m1 codes [128 tokens][64 bytes], two a byte along the head dimension. Every 32 elements share a power of two
+//           2^(b - 127); the bytes b lie at [block of 32][token % 16][token / 16], so that lane (l16, q4)
+//           gets those of its 8 tokens 16 i + l16 and its block q4 with one 8-byte load.
+//   values  e2m1 codes [128 elements][64 bytes], two a byte along the tokens: position 32 a + 4 b + c of a row
+//           is token 16 b + 4 a + c. That is the order in which the score products leave a lane's weights, so
+//           they enter the second product without a move between lanes.
+//           One scale per token (bf16 with 6 significant bits), in the same order: it goes into the
+//           weight, because the contraction runs over the tokens.
+// Codes times scales have at most 8 significant bits, so the bf16 operands of the products are exact.
+#include "common.hpp"
+#include "internal.hpp"
+#include "lds_limit.hpp"
+
+namespace attt {
+
+namespace {
+constexpr int DH = 128;
+constexpr int kPage = kKv4Page, kRec = kKv4Record;
+constexpr int kOffV = kPage * DH / 2, kOffKs = 2 * kOffV, kOffVs = kOffKs + kPage * 4;
+static_assert(kOffVs + kPage * 2 == kRec, "the record's parts");
+constexpr float kLog2e = 1.4426950408889634f;
+
+// Where token t of a page stands in a value row.
+__device__ __forceinline__ int value_pos(int t) { return 32 * ((t >> 2) & 3) + 4 * (t >> 4) + (t & 3); }
+
+// Sequence of workgroup `bid`: the last whose wg_begin is at most bid.
+__device__ __forceinline__ int find_seq(const Kv4Batch& b, int bid) {
+  const int lane = threadIdx.x & 63;
+  return __builtin_amdgcn_readfirstlane(__popcll(__ballot(lane < b.count && b.s[lane < b.count ? lane : 0].wg_begin <= bid)) - 1);
+}
+
+// e2m1 code of x: to nearest, ties to the even code, 6 at most; the sign of a zero is kept.
+__device__ __forceinline__ uint32_t e2m1(float x) {
+  const float a = fabsf(x);
+  const uint32_t mag = (a > 0.25f) + (a >= 0.75f) + (a > 1.25f) + (a >= 1.75f) + (a > 2.5f) + (a >= 3.5f) + (a > 5.0f);
+  return mag | (__float_as_uint(x) >> 28 & 8u);
+}
+__device__ __forceinline__ float e2m1_value(uint32_t c) {
+  const uint32_t m = c & 7u;
+  const float v = m < 4u ? 0.5f * (float)m : m == 4u ? 2.0f : m == 5u ? 3.0f : m == 6u ? 4.0f : 6.0f;
+  return c & 8u ? -v : v;
+}
+}  // namespace
+
+// The new rows of one (sequence, key/value head) that fall into one page. Sixteen lanes take a token, eight
+// elements each: the maxima of its key blocks (4 lanes) and of its value row (16 lanes) meet in shuffles. Key codes go
+// to the page at once; value codes are turned through LDS, and each 16-byte piece of a value row is
+// written by one thread, which keeps the codes of the tokens that were there.
+__global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Args a, Kv4Batch b) {
+  const Kv4Seq S = b.s[find_seq(b, blockIdx.x)];
+  const int local = (int)blockIdx.x - S.wg_begin;
+  const int kh = local % a.kv_heads;
+  const int64_t len = a.lengths[S.seq];
+  const int64_t first = len - S.n;  // position of the sequence's first new row; rows before 0 are not stored
+  const int64_t page = (first > 0 ? first : 0) / kPage + local / a.kv_heads;
+  const bool bad_len = len > a.width * kPage;
+  const int id = page < a.width && !bad_len && page * kPage < len ? a.table[S.seq * a.width + page] : -1;
+  const bool stored = id >= 0 && id < a.pages;
+  __shared__ __align__(16) uint8_t codes[DH][kPage + 16];  // value codes by (element, position); pitch 144
+  const int tid = threadIdx.x, lane16 = tid & 15;
+  const bool held = a.k_held != nullptr;
+  uint8_t* rec = a.cache + ((int64_t)(stored ? id : 0) * a.kv_heads + kh) * kRec;
+  // rows [i0, i1) of the sequence lie in this page
+  const int i0 = (int)max((int64_t)0, page * kPage - first), i1 = (int)min((int64_t)S.n, page * kPage + kPage - first);
+  if (local / a.kv_heads == 0 && held) {
+    // what the sequence has no place for: rows before its start hold nothing, those of a bad length NaN
+    const int none = bad_len ? S.n : (int)min((int64_t)S.n, max((int64_t)0, -first));
+    const uint32_t fill = bad_len ? 0x7FC07FC0u : 0u;
+    for (int i = tid >> 4; i < none; i += 16) {
+      const int64_t at = ((S.row0 + i) * a.kv_heads + kh) * DH + lane16 * 8;
+      *reinterpret_cast<u32x4*>(a.k_held + at) = u32x4{fill, fill, fill, fill};
+      *reinterpret_cast<u32x4*>(a.v_held + at) = u32x4{fill, fill, fill, fill};
+    }
+  }
+  if (bad_len || i0 >= i1) return;
+  for (int i = i0 + (tid >> 4); i - (tid >> 4) < i1; i += 16) {
+    const bool on = i < i1;
+    const int64_t at = ((S.row0 + (on ? i : i0)) * a.kv_heads + kh) * DH + lane16 * 8;
+    const u32x4 xk = *reinterpret_cast<const u32x4*>(a.k + at), xv = *reinterpret_cast<const u32x4*>(a.v + at);
+    float fk[8], fv[8];
+    uint32_t mk = 0, mv = 0;  // the largest magnitude, as bits: NaN above infinity above the rest
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      fk[e] = bf16_bits_to_f32(xk[e >> 1] >> (e & 1 ? 16 : 0) & 0xFFFFu);
+      fv[e] = bf16_bits_to_f32(xv[e >> 1] >> (e & 1 ? 16 : 0) & 0xFFFFu);
+      mk = max(mk, __float_as_uint(fk[e]) & 0x7FFFFFFFu);
+      mv = max(mv, __float_as_uint(fv[e]) & 0x7FFFFFFFu);
+    }
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) {
+      if (o < 4) mk = max(mk, (uint32_t)__shfl_xor((int)mk, o, 64));
+      mv = max(mv, (uint32_t)__shfl_xor((int)mv, o, 64));
+    }
+    // keys: the power of two that leaves the largest of 32 below 7 (6, the largest code, is nearer to it than 8
+    // times half of it): the exponent, less 2, rounded up from 1.75; at least 2^-100, and 6 times it is finite.
+    const bool nan_k = mk >= 0x7F800000u, nan_v = mv >= 0x7F800000u;
+    const uint32_t ek = nan_k ? 255u : min(252, max(27, (int)((mk + 0x200000u) >> 23) - 2));
+    const float ik = __uint_as_float((254u - min(ek, 253u)) << 23);  // 2^(127 - ek), exact
+    // values: a sixth of the largest, rounded up to 6 significant bits, so that the largest is 6 at most
+    // (bounded like the keys')
+    const float sixth = __fdiv_rn(__uint_as_float(mv), 6.0f);
+    const float sv = nan_v ? __uint_as_float(0x7FC00000u)
+                           : fminf(fmaxf(__uint_as_float((__float_as_uint(sixth) + 0x3FFFFu) & ~0x3FFFFu), 0x1p-100f), 0x1.5p125f);
+    const int t = (int)(first + i - page * kPage);  // in the page
+    uint32_t ck[8], cv[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      ck[e] = nan_k ? 0u : e2m1(fk[e] * ik);
+      cv[e] = nan_v ? 0u : e2m1(__fdiv_rn(fv[e], sv));
+    }
+    if (on && stored) {
+      uint32_t w = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w |= ck[e] << (4 * e);
+      *reinterpret_cast<uint32_t*>(rec + t * 64 + lane16 * 4) = w;
+      if ((lane16 & 3) == 0) rec[kOffKs + (lane16 >> 2) * 128 + (t & 15) * 8 + (t >> 4)] = (uint8_t)ek;
+      const int p = value_pos(t);
+      if (lane16 == 0) *reinterpret_cast<uint16_t*>(rec + kOffVs + 2 * p) = (uint16_t)(__float_as_uint(sv) >> 16);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) codes[lane16 * 8 + e][p] = (uint8_t)cv[e];
+    }
+    if (on && held) {
+      const float sk = nan_k ? __uint_as_float(0x7FC00000u) : __uint_as_float(ek << 23);
+      const float pv = stored ? sv : __uint_as_float(0x7FC00000u), pk = stored ? sk : __uint_as_float(0x7FC00000u);
+      u32x4 hk, hv;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        hk[e] = pack_bf16x2(e2m1_value(ck[2 * e]) * pk, e2m1_value(ck[2 * e + 1]) * pk);
+        hv[e] = pack_bf16x2(e2m1_value(cv[2 * e]) * pv, e2m1_value(cv[2 * e + 1]) * pv);
+      }
+      *reinterpret_cast<u32x4*>(a.k_held + at) = hk;
+      *reinterpret_cast<u32x4*>(a.v_held + at) = hv;
+    }
+  }
+  if (!stored) return;
+  __syncthreads();
+  const int t0 = (int)(first + i0 - page * kPage), t1 = (int)(first + i1 - page * kPage);  // tokens [t0, t1) are new
+  for (int j = tid; j < DH * 4; j += 256) {
+    const int d = j >> 2, q = j & 3;  // positions 32 q .. +31: tokens 16 i + 4 q + r
+    u32x4* dst = reinterpret_cast<u32x4*>(rec + kOffV + d * 64 + q * 16);
+    u32x4 keep = u32x4{0, 0, 0, 0}, w = u32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int t = 16 * i + 4 * q + r, s = 16 * (i & 1) + 4 * r;
+        if (t >= t0 && t < t1)
+          w[i >> 1] |= (uint32_t)codes[d][32 * q + 4 * i + r] << s;
+        else
+          keep[i >> 1] |= 0xFu << s;
+      }
+    const bool all = (keep[0] | keep[1] | keep[2] | keep[3]) == 0u;
+    if ((keep[0] & keep[1] & keep[2] & keep[3]) == 0xFFFFFFFFu) continue;  // none of the new tokens
+    if (!all) w |= *dst & keep;
+    *dst = w;
+  }
+}
+
+// Attention of the new tokens of one (sequence, key/value head) over pages [split chunk, ..) of the sequence.
+// A wave takes whole pages in turn with the other three. The query rows of the head's group (token i,
+// query head j: row i g + j) are the columns of S^T = K Q^T, RT tiles of 16, so each lane holds scores of its own rows
+// only; per page the online softmax is a reduction over the lane's registers and its three partner
+// lanes. Weight times value scale, rounded to bf16 once, is the B operand of O^T = V^T P^T. A page's
+// keys are asked for while the one before is multiplied with its values, and its values while its keys
+// are. At the end the waves' sums are joined in a fixed order through LDS.
+template <int RT>
+__global__ __launch_bounds__(256) void kv4_attention_kernel(Kv4Args a, Kv4Batch b) {
+  constexpr int R = 16 * RT;
+  const Kv4Seq S = b.s[find_seq(b, blockIdx.x)];
+  const int local = (int)blockIdx.x - S.wg_begin;
+  const int kh = local % a.kv_heads, sb = local / a.kv_heads;
+  const int split = sb % a.splits, rb = sb / a.splits;
+  const int g = a.heads / a.kv_heads;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l16 = lane & 15, q4 = lane >> 4;
+  int64_t len = a.lengths[S.seq];
+  bool bad = len > a.max_length;
+  if (len < 0 || bad) len = 0;
+  const int used = (int)((len + kPage - 1) / kPage);
+  const int p0 = split * a.chunk, p1 = min(used, p0 + a.chunk);
+  if (split > 0 && p0 >= p1) return;  // not among those that are joined
+  const int64_t first = len - S.n;  // position of the first new row
+  bf16x8 qf[RT][4];
+  int lim[RT];  // the last position that the lane's row sees; -1: none
+#pragma unroll
+  for (int c = 0; c < RT; ++c) {
+    const int row = rb * R + 16 * c + l16, i = row / g, j = row % g;
+    const bool on = row < S.n * g;
+    lim[c] = on ? (int)max((int64_t)-1, first + i) : -1;
+    const bf16_t* src = a.q + ((S.row0 + (on ? i : 0)) * a.heads + kh * g + (on ? j : 0)) * DH + 32 * q4;
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+      qf[c][s] = on ? __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(src + 8 * s)) : bf16x8{};
+  }
+  // every row of the block sees the positions up to here
+  const int64_t all_see = first + (rb * R) / g;
+  const float sl = a.scale * kLog2e;
+  float m[RT], l[RT];
+  f32x4 o[RT][8];
+#pragma unroll
+  for (int c = 0; c < RT; ++c) {
+    m[c] = -INFINITY, l[c] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[c][j] = f32x4{0, 0, 0, 0};
+  }
+  u32x4 kr[8], vr[8], vs[4];
+  uint2 ks;
+  const int32_t* table = a.table + (int64_t)S.seq * a.width;
+  auto record = [&](int p) -> const uint8_t* {
+    int id = table[p];
+    if (id < 0 || id >= a.pages) bad = true, id = 0;
+    return a.cache + ((int64_t)id * a.kv_heads + kh) * kRec;
+  };
+  auto load_k = [&](const uint8_t* rec) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) kr[i] = *reinterpret_cast<const u32x4*>(rec + (16 * i + l16) * 64 + 16 * q4);
+    ks = *reinterpret_cast<const uint2*>(rec + kOffKs + 128 * q4 + 8 * l16);
+  };
+  auto load_v = [&](const uint8_t* rec) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) vr[j] = *reinterpret_cast<const u32x4*>(rec + kOffV + (16 * j + l16) * 64 + 16 * q4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) vs[i] = *reinterpret_cast<const u32x4*>(rec + kOffVs + 64 * q4 + 16 * i);
+  };
+  // eight e2m1 codes times a scale as bf16 (exact)
+  auto widen = [](uint32_t x, float scale) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    bf16x2 y[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 0), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 1),
+                   __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 2), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 3)};
+    return bf16x8{y[0][0], y[0][1], y[1][0], y[1][1], y[2][0], y[2][1], y[3][0], y[3][1]};
+  };
+  int p = p0 + w;
+  const uint8_t* rec = nullptr;
+  if (p < p1) {
+    rec = record(p);
+    load_k(rec);
+    load_v(rec);
+  }
+  for (; p < p1; p += 4) {
+    const bool more = p + 4 < p1;
+    const uint8_t* next = more ? record(p + 4) : rec;
+    f32x4 st[RT][8];  // S^T[16 i + 4 q4 + r][row]
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+#pragma unroll
+      for (int c = 0; c < RT; ++c) st[c][i] = f32x4{0, 0, 0, 0};
+      const float sc = __uint_as_float(((i < 4 ? ks.x : ks.y) >> (8 * (i & 3)) & 255u) << 23);
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const bf16x8 ak = widen(kr[i][s], sc);
+#pragma unroll
+        for (int c = 0; c < RT; ++c) st[c][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ak, qf[c][s], st[c][i], 0, 0, 0);
+      }
+    }
+    if (more) load_k(next);
+    const int t0 = p * kPage + 4 * q4;  // the lane's tokens: t0 + 16 i + r
+    bf16x8 pw[RT][4];
+    auto softmax = [&](auto masked) {
+#pragma unroll
+      for (int c = 0; c < RT; ++c) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            float v = st[c][i][r] * sl;
+            if constexpr (decltype(masked)::value) v = t0 + 16 * i + r <= lim[c] ? v : -INFINITY;
+            st[c][i][r] = v;
+            mx = fmaxf(mx, v);
+          }
+        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        if (__any(mx > m[c] + 8.0f)) {
+          const float mn = mx > m[c] + 8.0f ? mx : m[c];  // per row: no other row of the tile changes it
+          const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[c] - mn);
+          m[c] = mn;
+          l[c] *= alpha;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) o[c][j] *= alpha;
+        }
+        const float ms = m[c] == -INFINITY ? 0.0f : m[c];
+        float sum = 0.0f;
+        u32x4 pk[4];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          float x[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float e = __builtin_amdgcn_exp2f(st[c][i][r] - ms);
+            sum += e;
+            const float scale = bf16_bits_to_f32(vs[i >> 1][(i & 1) * 2 + (r >> 1)] >> (r & 1 ? 16 : 0) & 0xFFFFu);
+            x[r] = e * scale;
+            // places that no token was written to hold any bits
+            if constexpr (decltype(masked)::value) x[r] = t0 + 16 * i + r <= lim[c] ? x[r] : 0.0f;
+          }
+          pk[i >> 1][(i & 1) * 2] = pack_bf16x2(x[0], x[1]);
+          pk[i >> 1][(i & 1) * 2 + 1] = pack_bf16x2(x[2], x[3]);
+        }
+        l[c] += sum;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) pw[c][u] = __builtin_bit_cast(bf16x8, pk[u]);
+      }
+    };
+    if ((int64_t)p * kPage + kPage - 1 <= all_see)
+      softmax(std::false_type{});
+    else
+      softmax(std::true_type{});
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const bf16x8 av = widen(vr[j][u], 1.0f);
+#pragma unroll
+        for (int c = 0; c < RT; ++c) o[c][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, pw[c][u], o[c][j], 0, 0, 0);
+      }
+    if (more) load_v(next);
+    rec = next;
+  }
+  // the four waves' maxima, sums and O: waves 2 and 3 hand over to 0 and 1, then 1 to 0
+  extern __shared__ __align__(16) uint8_t smem[];  // two waves' O, then their (m, l)
+  f32x4* ex = reinterpret_cast<f32x4*>(smem);
+  float2* ml = reinterpret_cast<float2*>(smem + 2 * (size_t)RT * 8 * 64 * sizeof(f32x4));
+#pragma unroll
+  for (int c = 0; c < RT; ++c) {
+    l[c] += __shfl_xor(l[c], 16, 64);
+    l[c] += __shfl_xor(l[c], 32, 64);
+    if (bad) l[c] = __uint_as_float(0x7FC00000u);
+  }
+#pragma unroll
+  for (int step = 2; step > 0; step >>= 1) {
+    __syncthreads();
+    if (w >= step && w < 2 * step) {
+#pragma unroll
+      for (int c = 0; c < RT; ++c) {
+        ml[((w - step) * RT + c) * 64 + lane] = make_float2(m[c], l[c]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) ex[(((w - step) * RT + c) * 8 + j) * 64 + lane] = o[c][j];
+      }
+    }
+    __syncthreads();
+    if (w < step) {
+#pragma unroll
+      for (int c = 0; c < RT; ++c) {
+        const float2 other = ml[(w * RT + c) * 64 + lane];
+        const float mn = fmaxf(m[c], other.x), ms = mn == -INFINITY ? 0.0f : mn;
+        const float fa = __builtin_amdgcn_exp2f(m[c] - ms), fb = __builtin_amdgcn_exp2f(other.x - ms);
+        m[c] = mn;
+        l[c] = l[c] * fa + other.y * fb;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[c][j] = o[c][j] * fa + ex[((w * RT + c) * 8 + j) * 64 + lane] * fb;
+      }
+    }
+  }
+  if (w != 0) return;
+  const int64_t unit = ((int64_t)(S.blk0 + rb) * a.kv_heads + kh) * a.splits + split;
+#pragma unroll
+  for (int c = 0; c < RT; ++c) {
+    const int row = rb * R + 16 * c + l16, i = row / g, j0 = row % g;
+    if (row >= S.n * g) continue;
+    if (a.splits > 1) {
+      float* po = a.part + (unit * R + 16 * c + l16) * DH;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) *reinterpret_cast<f32x4*>(po + 16 * j + 4 * q4) = o[c][j];
+      if (q4 == 0) a.part_ml[unit * R + 16 * c + l16] = make_float2(m[c], l[c]);
+      continue;
+    }
+    const int64_t at = (S.row0 + i) * a.heads + kh * g + j0;
+    const float inv = l[c] == 0.0f ? 0.0f : 1.0f / l[c];  // a row that sees nothing: 0, lse -inf
+    if (q4 == 0) a.lse[(int64_t)(kh * g + j0) * a.N + S.row0 + i] = l[c] == 0.0f ? -INFINITY : m[c] / kLog2e + logf(l[c]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      *reinterpret_cast<uint2*>(a.o + at * DH + 16 * j + 4 * q4) =
+          make_uint2(pack_bf16x2(o[c][j][0] * inv, o[c][j][1] * inv), pack_bf16x2(o[c][j][2] * inv, o[c][j][3] * inv));
+  }
+}
+
+// Joins the splits of a row in their order. One wave per (row, query head), two elements a lane.
+template <int RT>
+__global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Args a, Kv4Batch b, int64_t rows) {
+  constexpr int R = 16 * RT;
+  const int lane = threadIdx.x & 63;
+  const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);  // (row of the batch, head)
+  if (at >= rows * a.heads) return;
+  const int64_t row = b.s[0].row0 + at / a.heads;
+  const int h = (int)(at % a.heads), g = a.heads / a.kv_heads;
+  // rows of empty sequences do not exist, so the last sequence that begins at or before the row holds it
+  const int e = __popcll(__ballot(lane < b.count && b.s[lane < b.count ? lane : 0].row0 <= row)) - 1;
+  const Kv4Seq S = b.s[e];
+  const int r = (int)(row - S.row0) * g + h % g;
+  int64_t len = a.lengths[S.seq];
+  if (len < 0 || len > a.max_length) len = 0;  // of a bad length the first split's sum is NaN
+  const int used = (int)((len + kPage - 1) / kPage);
+  const int ns = max(1, (used + a.chunk - 1) / a.chunk);
+  const int64_t unit = ((int64_t)(S.blk0 + r / R) * a.kv_heads + h / g) * a.splits;
+  float m = -INFINITY, l = 0.0f;
+  float2 o = make_float2(0.0f, 0.0f);
+#pragma unroll 4
+  for (int s = 0; s < ns; ++s) {
+    const int64_t u = (unit + s) * R + r % R;
+    const float2 ml = a.part_ml[u];
+    const float2 x = *reinterpret_cast<const float2*>(a.part + u * DH + 2 * lane);
+    const float mn = fmaxf(m, ml.x), ms = mn == -INFINITY ? 0.0f : mn;
+    const float fa = __builtin_amdgcn_exp2f(m - ms), fb = __builtin_amdgcn_exp2f(ml.x - ms);
+    m = mn;
+    l = l * fa + ml.y * fb;
+    o.x = o.x * fa + x.x * fb;
+    o.y = o.y * fa + x.y * fb;
+  }
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  if (lane == 0) a.lse[(int64_t)h * a.N + row] = l == 0.0f ? -INFINITY : m / kLog2e + logf(l);
+  *reinterpret_cast<uint32_t*>(a.o + (row * a.heads + h) * DH + 2 * lane) = pack_bf16x2(o.x * inv, o.y * inv);
+}
+
+hipError_t launch_kv4_append(const Kv4Args& a, Kv4Batch b, hipStream_t s) {
+  int64_t n = 0;
+  for (int i = 0; i < b.count; ++i) {
+    b.s[i].wg_begin = (int32_t)n;
+    if (b.s[i].n > 0) n += (int64_t)((b.s[i].n + kPage - 2) / kPage + 1) * a.kv_heads;
+  }
+  if (n <= 0) return hipSuccess;
+  KernelTimer t(K_KV4_APPEND, s);
+  hipLaunchKernelGGL(kv4_append_kernel, dim3((unsigned)n), dim3(256), 0, s, a, b);
+  return hipGetLastError();
+}
+
+template <int RT>
+static hipError_t launch_rows(LdsLimit& limit, const Kv4Args& a, Kv4Batch b, hipStream_t s) {
+  constexpr size_t lds = 2 * (size_t)RT * 8 * 64 * sizeof(f32x4) + 2 * (size_t)RT * 64 * sizeof(float2);
+  if (hipError_t e = limit.raise((const void*)kv4_attention_kernel<RT>, lds)) return e;
+  const int g = a.heads / a.kv_heads;
+  int64_t n = 0, rows = 0;
+  for (int i = 0; i < b.count; ++i) {
+    const int64_t blocks = ((int64_t)b.s[i].n * g + 16 * RT - 1) / (16 * RT);
+    b.s[i].wg_begin = (int32_t)n;
+    n += blocks * a.kv_heads * a.splits;
+    rows += b.s[i].n;
+  }
+  if (n <= 0) return hipSuccess;
+  {
+    KernelTimer t(K_KV4_ATTN, s);
+    hipLaunchKernelGGL(kv4_attention_kernel<RT>, dim3((unsigned)n), dim3(256), lds, s, a, b);
+  }
+  if (a.splits > 1) {
+    KernelTimer t(K_KV4_JOIN, s);
+    hipLaunchKernelGGL(kv4_join_kernel<RT>, dim3((unsigned)((rows * a.heads + 3) / 4)), dim3(256), 0, s, a, b, rows);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_kv4_attention(int row_tiles, const Kv4Args& a, const Kv4Batch& b, hipStream_t s) {
+  static LdsLimit limits[3];
+  return row_tiles == 1   ? launch_rows<1>(limits[0], a, b, s)
+         : row_tiles == 2 ? launch_rows<2>(limits[1], a, b, s)
+                          : launch_rows<4>(limits[2], a, b, s);
+}
+
+}  // namespace attt

@@ -1,0 +1,249 @@
+"""GPU parity of the prompt attention's forward and of the backward that reads what it saved, against float64.
+
+The output's bound counts its two bf16 roundings (2^-8 each at most): every softmax weight is rounded once, which
+moves an output by at most 2^-8 sum p|v|, and the output itself by 2^-8 of its size; the
+float32 sums add far less than the 1% that the bound is widened by. lse's counts float32 steps: a score is a sum of 128
+exact products, scaled twice, and the softmax sum has at most the row's number of terms."""
+import numpy as np
+import pytest
+
+from gpu_util import check_rows, dev_dense, host, note
+from oracle import attention as oat
+from workloads.gen import random_dense
+
+pytestmark = pytest.mark.gpu
+DH = 128
+
+
+def inputs(N, H, kv, seed, std=1.0):
+    return (random_dense((N, H, DH), std, True, seed), random_dense((N, kv, DH), std, True, seed + 1),
+            random_dense((N, kv, DH), 1.0, True, seed + 2), random_dense((N, H, DH), 0.05, True, seed + 3))
+
+
+def absolute(q, k, v, off):
+    """sum p |v| [N, H, 128] and, per (head, row), the largest sum |q||k| of the visible keys."""
+    N, H = q.shape[:2]
+    a = oat.attention_fwd_bwd(q, k, np.abs(v), np.zeros_like(q), off)["O"]
+    size = np.zeros((H, N))
+    g = H // k.shape[1]
+    for s, e in zip(off[:-1], off[1:]):
+        for h in range(H):
+            if e > s:
+                x = np.tril(np.abs(q[s:e, h]) @ np.abs(k[s:e, h // g]).T)
+                size[h, s:e] = x.max(1)
+    return a, size
+
+
+def check_forward(o, lse, q, k, v, off, scale=None):
+    q, k, v = (np.asarray(x, np.float64) for x in (q, k, v))
+    r = oat.attention_fwd_bwd(q, k, v, np.zeros_like(q), off, scale)
+    sc = 1.0 / np.sqrt(DH) if scale is None else scale
+    a, size = absolute(q * sc * np.sqrt(DH), k, v, off)
+    err = np.abs(o - r["O"])
+    bound = 1.01 * 2.0 ** -8 * (a + np.abs(r["O"])) + 2.0 ** -126
+    note(f"o: largest error over its bound {float((err / bound).max()):.3f}")
+    assert (err <= bound).all()
+    # 2^-24 x (128 sums and 2 scalings of the score, a sum of at most N terms, exp2, log, the last sum)
+    bl = 2.0 ** -24 * (132 * size / np.sqrt(DH) + 4 * np.abs(r["lse"]) + np.diff(off).max() + 16)
+    e2 = np.abs(lse - r["lse"])
+    note(f"lse: largest error over its bound {float((e2 / bl).max()):.3f}")
+    assert (e2 <= bl).all()
+    return r
+
+
+CASES = [  # heads, kv heads, episodes
+    (4, 4, [0, 1]), (4, 2, [0, 1, 65, 129, 200, 264, 300]), (8, 1, [0, 0, 3, 3, 130, 257, 257]),
+    (6, 2, [0, 63, 127, 191]), (5, 5, [0, 128]), (7, 1, [0, 129, 322]), (40, 8, [0, 513, 514, 900]),
+    (32, 4, [0, 700, 1500, 1601])]
+
+
+@pytest.mark.parametrize("H,kv,off", CASES)
+def test_forward(attt, H, kv, off):
+    off = np.array(off, np.int64)
+    N = int(off[-1])
+    note(f"attention_fwd: {H} heads over {kv}, episodes {np.diff(off).tolist()}")
+    q, k, v, _ = inputs(N, H, kv, 100 + H + N)
+    o, lse = attt.attention_fwd(dev_dense(q), dev_dense(k), dev_dense(v), row_offsets=off)
+    check_forward(host(o), host(lse), q.f32, k.f32, v.f32, off)
+
+
+def test_many_query_tiles(attt):
+    """Workgroups of 128 queries: episodes that end on and beside the edges of its blocks and waves."""
+    lens = [1, 31, 33, 63, 64, 65, 97, 127, 128, 129, 191, 192, 193, 200, 256, 257, 130, 0, 5]
+    off = np.concatenate([[0], np.cumsum(lens)]).astype(np.int64)
+    H, kv = 24, 3
+    assert sum((n + 127) // 128 for n in lens) * H > 480
+    note(f"attention_fwd: {H} heads, episodes {lens}")
+    q, k, v, _ = inputs(int(off[-1]), H, kv, 7)
+    o, lse = attt.attention_fwd(dev_dense(q), dev_dense(k), dev_dense(v), row_offsets=off)
+    check_forward(host(o), host(lse), q.f32, k.f32, v.f32, off)
+
+
+def test_more_episodes_than_a_launch(attt):
+    off = np.arange(151, dtype=np.int64) * 3
+    q, k, v, _ = inputs(450, 2, 1, 9)
+    o, lse = attt.attention_fwd(dev_dense(q), dev_dense(k), dev_dense(v), row_offsets=off)
+    check_forward(host(o), host(lse), q.f32, k.f32, v.f32, off)
+
+
+@pytest.mark.parametrize("std,scale", [(6.0, None), (1.0, 1.0), (1.0, 1e-3)])
+def test_peaked_and_flat(attt, std, scale):
+    """Scores of several hundred, where the maximum grows step by step, and rows that are nearly uniform."""
+    off = np.array([0, 400], np.int64)
+    q, k, v, _ = inputs(400, 4, 2, 31, std)
+    o, lse = attt.attention_fwd(dev_dense(q), dev_dense(k), dev_dense(v), scale=scale)
+    check_forward(host(o), host(lse), q.f32, k.f32, v.f32, off, scale)
+
+
+def test_growing_scores(attt):
+    """Keys in the order of their scores: the running maximum is replaced in every block."""
+    import torch
+    N = 640
+    k = torch.zeros(N, 1, DH, dtype=torch.bfloat16, device="cuda")
+    k[:, 0, 0] = torch.linspace(-40.0, 40.0, N, device="cuda").bfloat16()
+    q = torch.zeros(N, 2, DH, dtype=torch.bfloat16, device="cuda")
+    q[:, 0, 0], q[:, 1, 0] = 30.0, -30.0
+    v = torch.randn(N, 1, DH, device="cuda", generator=torch.Generator("cuda").manual_seed(3)).bfloat16()
+    o, lse = attt.attention_fwd(q, k, v)
+    check_forward(host(o), host(lse), host(q), host(k), host(v), np.array([0, N]))
+
+
+def test_nonfinite_in_masked_places(attt):
+    """A NaN or an infinity in a later token's key or value, or in another episode, changes no bit before it."""
+    import torch
+    off = np.array([0, 100, 300], np.int64)
+    q, k, v, _ = (dev_dense(x) for x in inputs(300, 4, 2, 17))
+    o0, l0 = attt.attention_fwd(q, k, v, row_offsets=off)
+    for at, what in ((70, float("nan")), (70, float("inf")), (99, float("-inf")), (250, float("nan"))):
+        end = 100 if at < 100 else 300
+        for side in (0, 1):
+            kv = [k.clone(), v.clone()]
+            kv[side][at, 0, 5] = what
+            o, lse = attt.attention_fwd(q, kv[0], kv[1], row_offsets=off)
+            seen = torch.zeros(300, dtype=torch.bool, device="cuda")
+            seen[at:end] = True
+            note(f"{what} in {'kv'[side]} of row {at}")
+            assert torch.equal(o[~seen], o0[~seen]) and torch.equal(lse[:, ~seen], l0[:, ~seen])
+            assert torch.equal(o[:, 2:], o0[:, 2:])  # the other key/value head's queries
+            if side == 1:
+                assert not torch.isfinite(o[seen][:, :2, 5]).any() and torch.equal(lse, l0)
+                rest = [c for c in range(DH) if c != 5]
+                assert torch.equal(o[:, :, rest], o0[:, :, rest])
+            elif what != what:
+                assert torch.isnan(o[seen][:, :2]).all() and torch.isnan(lse[:2, seen]).all()
+
+
+def test_minus_infinity_scores_first(attt):
+    """The first keys' scores are -inf: they have no weight, and the finite ones behind them all of it."""
+    import torch
+    N = 200
+    q, k, v, _ = (dev_dense(x) for x in inputs(N, 1, 1, 5))
+    q[:, 0, 0] = 1.0
+    k[:130, 0, 0] = float("-inf")
+    o, lse = attt.attention_fwd(q, k, v)
+    assert torch.isnan(o[:130]).all()
+    q64, k64, v64 = (x[:, 0].double().cpu().numpy() for x in (q, k, v))
+    s = np.tril(q64[130:] @ k64[130:].T) / np.sqrt(DH)
+    e = np.tril(np.exp(s))
+    want = (e / e.sum(1, keepdims=True)) @ v64[130:]
+    a = (e / e.sum(1, keepdims=True)) @ np.abs(v64[130:])
+    assert (np.abs(host(o)[130:, 0] - want) <= 1.01 * 2.0 ** -8 * (a + np.abs(want))).all()
+
+
+@pytest.mark.parametrize("H,kv,off", [(4, 2, [0, 1, 65, 129, 200, 264, 300]), (8, 1, [0, 0, 3, 130, 257]),
+                                      (16, 4, [0, 2048]), (8, 8, [0, 300, 301, 640])])
+def test_saved_backward(attt, H, kv, off):
+    """Against float64, with the bounds of the backward that computes its own statistics; dsum counts O's
+    rounding: at most 2^-8 sum |dO||O|, and the weights' 2^-8 sum |dO| sum p|v|."""
+    off = np.array(off, np.int64)
+    N = int(off[-1])
+    note(f"attention_bwd_saved: {H} heads over {kv}, episodes {np.diff(off).tolist()}")
+    q, k, v, do = inputs(N, H, kv, 300 + H)
+    dq_, dk_, dv_, ddo = (dev_dense(x) for x in (q, k, v, do))
+    o, lse = attt.attention_fwd(dq_, dk_, dv_, row_offsets=off)
+    o_before, lse_before = o.clone(), lse.clone()
+    dq, dk, dv, dsum = attt.attention_bwd_saved(dq_, dk_, dv_, o, lse, ddo, row_offsets=off)
+    assert o.equal(o_before) and lse.equal(lse_before)
+    r = oat.attention_fwd_bwd(q.f32, k.f32, v.f32, do.f32, off)
+    a, _ = absolute(np.float64(q.f32), np.float64(k.f32), np.float64(v.f32), off)
+    # D's rounding error reaches dQ = scale P (dP - D) K through sum_s P K, and dK through Q: 2^-7 of the rows'
+    # sizes is the bound of the backward without it, to which the rounding's own share is added
+    dd = 2.0 ** -7 * (np.abs(do.f32) * a).sum(2).T
+    assert (np.abs(host(dsum) - r["D"]) <= 1.01 * dd).all()
+    sc = 1.0 / np.sqrt(DH)
+    g = H // kv
+    more_q, more_k = np.zeros(q.f32.shape), np.zeros(k.f32.shape)
+    for s, e in zip(off[:-1], off[1:]):
+        for h in range(H):
+            if e == s:
+                continue
+            x = np.where(np.tril(np.ones((e - s, e - s), bool)), sc * (np.float64(q.f32[s:e, h]) @ np.float64(k.f32[s:e, h // g]).T), -np.inf)
+            p = np.exp(x - x.max(1, keepdims=True))
+            p = p / p.sum(1, keepdims=True) * dd[h, s:e, None] * sc
+            more_q[s:e, h] = p @ np.abs(k.f32[s:e, h // g])
+            more_k[s:e, h // g] += p.T @ np.abs(q.f32[s:e, h])
+    for name, got, want, more in (("dQ", dq, r["dQ"], more_q), ("dK", dk, r["dK"], more_k), ("dV", dv, r["dV"], 0.0)):
+        got = host(got)
+        size = np.sqrt(np.mean(want ** 2, axis=-1, keepdims=True))
+        bound = 2.0 ** -7 * (np.abs(want) + size + 2.0 ** -7 * np.sqrt(np.mean(want ** 2))) + more
+        note(f"{name}: largest error over its bound {float((np.abs(got - want) / bound).max()):.3f}")
+        assert (np.abs(got - want) <= bound).all(), name
+    # without a workspace: one workgroup per key block
+    import ctypes
+    L = attt.load()
+    alone = [dq.clone(), dk.clone(), dv.clone(), dsum.clone()]
+    oo, op = attt._offsets(off)
+    attt._check(L.attt_attention_bwd_saved(*(x.data_ptr() for x in (dq_, dk_, dv_, o, lse, ddo)), op, len(off) - 1, N, H, kv, DH,
+                                           ctypes.c_float(sc), *(x.data_ptr() for x in alone), None, 0, attt._stream_ptr()))
+    check_rows(host(alone[0]).reshape(N, -1), host(dq).reshape(N, -1), 0.999, 2.0 ** -6, "dQ without a workspace")
+    assert alone[3].equal(dsum)
+
+
+def test_gradient_against_differences(attt):
+    """Central differences of sum(dout * O) in float64 along random directions, for inputs that bf16 holds."""
+    off = np.array([0, 33, 100], np.int64)
+    q, k, v, do = inputs(100, 4, 2, 77)
+    t = [dev_dense(x) for x in (q, k, v)]
+    o, lse = attt.attention_fwd(*t, row_offsets=off)
+    g = [host(x).astype(np.float64) for x in attt.attention_bwd_saved(*t, o, lse, dev_dense(do), row_offsets=off)[:3]]
+    x = [np.float64(y.f32) for y in (q, k, v)]
+    rng = np.random.default_rng(5)
+    h = 1e-5
+    for i in range(3):
+        d = rng.standard_normal(x[i].shape)
+        f = [float((oat.attention_fwd_bwd(*(x[j] + (s * h * d if j == i else 0) for j in range(3)), np.float64(do.f32), off)["O"]
+                    * do.f32).sum()) for s in (1, -1)]
+        want = (f[0] - f[1]) / (2 * h)
+        # the gradients' bf16 roundings and those behind them, 2^-7 of each element along the direction
+        assert abs((g[i] * d).sum() - want) <= 2.0 ** -7 * np.sqrt(((np.abs(g[i]) + np.sqrt(np.mean(g[i] ** 2))) ** 2 * d ** 2).sum()) * 4, i
+
+
+def test_streams_graphs_and_repeats(attt):
+    """The same bits on another stream, in every replay of a captured graph, and with outputs given."""
+    import torch
+    off = [0, 90, 300]
+    q, k, v, do = (dev_dense(x) for x in inputs(300, 8, 2, 51))
+    o, lse = attt.attention_fwd(q, k, v, row_offsets=off)
+    grads = attt.attention_bwd_saved(q, k, v, o, lse, do, row_offsets=off)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        o2, l2 = attt.attention_fwd(q, k, v, row_offsets=np.array(off, np.int64))
+        g2 = attt.attention_bwd_saved(q, k, v, o2, l2, do, row_offsets=tuple(off))
+    torch.cuda.current_stream().wait_stream(s)
+    assert o2.equal(o) and l2.equal(lse) and all(a.equal(b) for a, b in zip(grads, g2))
+    out = (torch.empty_like(o), torch.empty_like(lse))
+    gout = tuple(torch.empty_like(x) for x in grads)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        attt.attention_fwd(q, k, v, row_offsets=off, out=out)
+        attt.attention_bwd_saved(q, k, v, *out, do, row_offsets=off, out=gout)
+    for n in range(3):
+        for x in (*out, *gout):
+            x.zero_()
+        q.copy_(torch.roll(q, n, 0))
+        want = attt.attention_fwd(q, k, v, row_offsets=off)
+        want = (*want, *attt.attention_bwd_saved(q, k, v, *want, do, row_offsets=off))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(a.equal(b) for a, b in zip((*out, *gout), want)), n

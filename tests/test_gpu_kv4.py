@@ -1,0 +1,335 @@
+"""The paged 4-bit cache on the GPU: its bytes bit for bit against the oracle, and the attention over it against
+float64 on the values that the bytes stand for.
+
+The attention's bound counts its two bf16 roundings (2^-8 each at most): weight times value scale moves an output by at
+most 2^-8 sum p|v|, the output itself by 2^-8 of its size; 1% more for the float32 sums. lse's counts
+float32 steps as for the prompt attention."""
+import numpy as np
+import pytest
+
+from gpu_util import host, note
+from oracle import kv4 as okv
+
+pytestmark = pytest.mark.gpu
+DH = 128
+
+
+def make(lengths, rows, H, kv, seed, std=1.0, extra=4, held_back=True):
+    """Random rows for `rows[e]` new tokens of each sequence of `lengths[e]`, and a cache that holds the others."""
+    import torch
+    rng = np.random.default_rng(seed)
+    E = len(lengths)
+    used = [(max(n, 0) + 127) // 128 for n in lengths]
+    pages = sum(used) + extra
+    order = rng.permutation(pages)
+    width = max(1, max(used)) + 1
+    table = np.full((E, width), -1, np.int32)
+    cache = np.full((pages, kv, okv.RECORD), 255, np.uint8)  # places that no token was written to hold NaN scales
+    a = 0
+    bf = lambda x: torch.from_numpy(np.ascontiguousarray(x, np.float32)).bfloat16().float().numpy()  # noqa: E731
+    hist = []
+    for e in range(E):
+        table[e, :used[e]] = order[a:a + used[e]]
+        a += used[e]
+        n = max(0, lengths[e] - rows[e])
+        k, v = bf(std * rng.standard_normal((n, kv, DH))), bf(rng.standard_normal((n, kv, DH)))
+        for c in range(kv):
+            okv.store(cache, table[e], c, 0, k[:, c], v[:, c])
+        hist.append((k, v))
+    N = sum(rows)
+    return dict(cache=cache, table=table, lengths=np.array(lengths, np.int32), off=np.concatenate([[0], np.cumsum(rows)]).astype(np.int64),
+                q=bf(rng.standard_normal((N, H, DH))), k=bf(std * rng.standard_normal((N, kv, DH))), v=bf(rng.standard_normal((N, kv, DH))))
+
+
+def dev(s):
+    import torch
+    out = {n: torch.from_numpy(s[n]).cuda() for n in ("cache", "table", "lengths")}
+    out.update({n: torch.from_numpy(s[n]).bfloat16().cuda() for n in "qkv"})
+    return out
+
+
+def expected(s):
+    """The cache after the append, and the held values of the rows."""
+    cache = s["cache"].copy()
+    kv = s["k"].shape[1]
+    kh, vh = okv.quant_k(s["k"])[2], okv.quant_v(s["v"])[2]
+    for e, n in enumerate(s["lengths"]):
+        a, b = s["off"][e], s["off"][e + 1]
+        first = int(n) - int(b - a)
+        for c in range(kv):
+            okv.store(cache, s["table"][e], c, first, s["k"][a:b, c], s["v"][a:b, c])
+        none = min(int(b - a), max(0, -first))
+        kh[a:a + none], vh[a:a + none] = 0.0, 0.0
+    return cache, kh, vh
+
+
+def check_attention(s, cache, o, lse, scale=None):
+    N, H = s["q"].shape[:2]
+    kv = s["k"].shape[1]
+    sc = 1.0 / np.sqrt(DH) if scale is None else scale
+    worst = [0.0, 0.0]
+    for e, n in enumerate(s["lengths"]):
+        a, b = s["off"][e], s["off"][e + 1]
+        for c in range(kv):
+            K, V = okv.load(cache, s["table"][e], c, max(0, int(n)))
+            for i in range(a, b):
+                last = int(n) - int(b - a) + int(i - a)
+                for h in range(c * (H // kv), (c + 1) * (H // kv)):
+                    want, wl, mag, size = okv.attend(np.float64(s["q"][i, h]), K, V, last, sc)
+                    if last < 0:
+                        assert not o[i, h].any() and lse[h, i] == -np.inf
+                        continue
+                    bound = 1.01 * 2.0 ** -8 * (mag + np.abs(want)) + 2.0 ** -126
+                    bl = 2.0 ** -24 * (132 * size + 4 * abs(wl) + last + 64)
+                    worst = [max(worst[0], float((np.abs(o[i, h] - want) / bound).max())), max(worst[1], abs(lse[h, i] - wl) / bl)]
+    note(f"o and lse: largest error over its bound {worst[0]:.3f}, {worst[1]:.3f}")
+    assert worst[0] <= 1.0 and worst[1] <= 1.0
+
+
+def run(attt, s, **kw):
+    d = dev(s)
+    kh, vh = attt.kv4_append(d["cache"], d["k"], d["v"], d["table"], d["lengths"], row_offsets=s["off"], want_held=True)
+    o, lse = attt.kv4_attention(d["q"], d["cache"], d["table"], d["lengths"], row_offsets=s["off"], **kw)
+    return d["cache"].cpu().numpy(), host(kh), host(vh), host(o), host(lse)
+
+
+CASES = [  # lengths, rows, heads, kv heads
+    ([1], [1], 1, 1), ([128], [1], 4, 2), ([129], [1], 8, 1), ([2, 0, 300, 127], [1, 1, 1, 1], 4, 2),
+    ([5], [5], 2, 2), ([131, 3], [7, 3], 6, 2), ([400, 17, 0, 256], [130, 17, 2, 128], 4, 2),
+    ([300], [300], 3, 1), ([1000, 2], [9, 5], 16, 2), ([700], [33], 8, 8), ([513], [40], 5, 1), ([90], [2], 56, 8)]
+
+
+@pytest.mark.parametrize("lengths,rows,H,kv", CASES)
+def test_append_and_attention(attt, lengths, rows, H, kv):
+    note(f"kv4: lengths {lengths}, new rows {rows}, {H} heads over {kv}")
+    s = make(lengths, rows, H, kv, 1000 + sum(lengths) + H)
+    cache, kh, vh, o, lse = run(attt, s)
+    want, wk, wv = expected(s)
+    assert np.array_equal(cache, want)
+    assert np.array_equal(kh, wk) and np.array_equal(vh, wv)
+    check_attention(s, want, o, lse)
+
+
+def test_magnitudes(attt):
+    """Codes over the whole range of sizes: blocks of zeros, subnormal and huge values, ties between codes, single
+    outliers."""
+    s = make([256], [256], 2, 2, 3)
+    rng = np.random.default_rng(8)
+    ties = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0, 6.99, 7.0, 7.5])
+    for x in (s["k"], s["v"]):
+        x[0:8] = 0.0
+        x[8:16, :, 0::2] = -0.0
+        for i in range(16, 120):
+            x[i] *= 2.0 ** float(rng.integers(-120, 120))
+        x[120:200] = (rng.choice(ties, (80, 2, DH)) * rng.choice([-1, 1], (80, 2, DH)) * 2.0 ** rng.integers(-8, 8, (80, 1, 1)))
+        x[200:210] *= 2.0 ** -133
+        x[210] = 3.3895314e38
+        x[211:220, :, 7] = 1e4
+    import torch
+    for n in "kv":
+        s[n] = torch.from_numpy(s[n]).bfloat16().float().numpy()
+    cache, kh, vh, _, _ = run(attt, s)
+    want, wk, wv = expected(s)
+    assert np.array_equal(cache, want)
+    assert np.array_equal(kh, wk) and np.array_equal(vh, wv)
+    assert np.isfinite(kh).all() and np.isfinite(vh).all()
+
+
+def test_nonfinite_keys_and_values(attt):
+    """A NaN or an infinity makes its block of 32, or its value row, NaN: rows that see it are NaN, the others as ever."""
+    rows = 20
+    for side, at, what in (("k", 4, np.nan), ("k", 4, np.inf), ("v", 4, np.nan), ("v", 4, -np.inf), ("k", 19, np.nan)):
+        s = make([150], [rows], 4, 2, 21)
+        _, _, _, o0, l0 = run(attt, s)
+        s[side][at, 1, 40] = what
+        cache, kh, vh, o, lse = run(attt, s)
+        assert np.array_equal(cache, expected(s)[0])
+        held = kh if side == "k" else vh
+        assert np.isnan(held[at, 1, 32:64] if side == "k" else held[at, 1]).all() and np.isfinite(held[at, 0]).all()
+        note(f"{what} in {side} of new row {at}")
+        assert np.array_equal(o[:at], o0[:at]) and np.array_equal(o[:, :2], o0[:, :2])
+        assert np.isnan(o[at:, 2:]).all()
+        if side == "k":
+            assert np.isnan(lse[2:, at:]).all() and np.array_equal(lse[:, :at], l0[:, :at])
+
+
+def test_bad_lengths_and_pages(attt):
+    """A length beyond the bound, a page outside the cache: NaN for that sequence, nothing written, the others as ever."""
+    s = make([200, 130, 300, 50], [2, 1, 1, 2], 4, 2, 33)
+    cache0, kh0, vh0, o0, l0 = run(attt, s)
+    for what in ("length", "page", "negative page", "negative length"):
+        t = dict(s, table=s["table"].copy(), lengths=s["lengths"].copy())
+        if what == "length":
+            t["lengths"][1] = 128 * t["table"].shape[1] + 1
+        elif what == "negative length":
+            t["lengths"][1] = -5
+        else:
+            t["table"][1, 1] = len(s["cache"]) if what == "page" else -7
+        note(f"kv4: bad {what}")
+        cache, kh, vh, o, lse = run(attt, t)
+        same = np.array([0, 1, 3, 4, 5])
+        for a, b in ((kh, kh0), (vh, vh0), (o, o0)):
+            assert np.array_equal(a[same], b[same])
+            if what == "negative length":
+                assert not a[2].any()
+            else:
+                assert np.isnan(a[2]).all()
+        assert np.array_equal(lse[:, same], l0[:, same])
+        assert (lse[:, 2] == -np.inf).all() if what == "negative length" else np.isnan(lse[:, 2]).all()
+        u = dict(s, off=s["off"])
+        want = s["cache"].copy()
+        for e in (0, 2, 3):
+            a, b = u["off"][e], u["off"][e + 1]
+            for c in range(2):
+                okv.store(want, s["table"][e], c, int(s["lengths"][e]) - int(b - a), s["k"][a:b, c], s["v"][a:b, c])
+        assert np.array_equal(cache, want)
+
+
+def test_max_length_below_a_length(attt):
+    s = make([200, 100], [1, 1], 2, 1, 35)
+    _, _, _, o0, _ = run(attt, s)
+    _, _, _, o, lse = run(attt, s, max_length=150)
+    assert np.isnan(o[0]).all() and np.isnan(lse[:, 0]).all()
+    # the other one is split otherwise: within two output roundings
+    assert (np.abs(o[1] - o0[1]) <= 2.0 ** -6 * (np.abs(o0[1]) + 1.0)).all()
+
+
+@pytest.mark.parametrize("rows,H,kv", [(1, 8, 2), (3, 8, 1), (17, 4, 1), (70, 4, 2)])
+def test_long_sequences_split(attt, rows, H, kv):
+    """Long and short sequences in one call, cut into many splits, on pages in any order."""
+    s = make([5000, 0, 1, 3333, 640, 7], [rows, rows, 1, rows, rows, 7], H, kv, 40 + rows)
+    note(f"kv4 splits: {rows} rows, {H} heads over {kv}")
+    assert attt.kv4_attention_workspace_size(int(s["off"][-1]), H, kv, 5000, row_offsets=s["off"]) > 0
+    cache, _, _, o, lse = run(attt, s, max_length=5000)
+    want, _, _ = expected(s)
+    assert np.array_equal(cache, want)
+    check_attention(s, want, o, lse)
+    _, _, _, o2, l2 = run(attt, s, max_length=5000)
+    assert np.array_equal(o, o2) and np.array_equal(lse, l2)  # bitwise repeatable
+
+
+def test_more_sequences_than_a_launch(attt):
+    lengths = [(37 * e) % 200 for e in range(131)]
+    s = make(lengths, [1] * 131, 2, 1, 61)
+    cache, _, _, o, lse = run(attt, s)
+    assert np.array_equal(cache, expected(s)[0])
+    check_attention(s, cache, o, lse)
+    d = dev(dict(s, cache=cache))
+    o2, l2 = attt.kv4_attention(d["q"], d["cache"], d["table"], d["lengths"])  # one row each without offsets
+    assert np.array_equal(host(o2), o) and np.array_equal(host(l2), lse)
+
+
+def test_beyond_32_bits(attt):
+    """Pages whose records begin past 4 GiB."""
+    import torch
+    kv, pages = 8, 33000
+    assert pages * kv * okv.RECORD > 1 << 32
+    s = make([260, 140], [3, 140], 16, kv, 71)
+    small = s["cache"]
+    cache = torch.zeros((pages, kv, okv.RECORD), dtype=torch.uint8, device="cuda")
+    cache[pages - len(small):] = torch.from_numpy(small[::-1].copy()).cuda()
+    table = np.where(s["table"] >= 0, pages - 1 - s["table"], -1).astype(np.int32)
+    d = dev(s)
+    t = torch.from_numpy(table).cuda()
+    attt.kv4_append(cache, d["k"], d["v"], t, d["lengths"], row_offsets=s["off"])
+    o, lse = attt.kv4_attention(d["q"], cache, t, d["lengths"], row_offsets=s["off"])
+    want, _, _ = expected(s)
+    assert np.array_equal(cache[pages - len(small):].cpu().numpy()[::-1], want)
+    assert not cache[:pages - len(small)].any()
+    check_attention(s, want, host(o), host(lse))
+
+
+def test_captured_steps_follow_lengths(attt):
+    """A captured decoding step replayed as the sequences grow, with eager work between: each replay as the eager step."""
+    import torch
+    s = make([127, 0, 300], [1, 1, 1], 8, 2, 81)
+    width = s["table"].shape[1] + 1
+    table = np.full((3, width), -1, np.int32)
+    table[:, :-1] = s["table"]
+    spare = [p for p in range(len(s["cache"])) if p not in s["table"]]
+    table[0, 1], table[1, 0] = spare[0], spare[1]
+    d = dev(dict(s, table=table))
+    out = (torch.empty_like(d["q"]), torch.empty(8, 3, device="cuda"))
+    ws = torch.empty(attt.kv4_attention_workspace_size(3, 8, 2, 512), dtype=torch.uint8, device="cuda")
+    step = lambda c, o: (attt.kv4_append(c, d["k"], d["v"], d["table"], d["lengths"]),  # noqa: E731
+                         attt.kv4_attention(d["q"], c, d["table"], d["lengths"], max_length=512, out=o, workspace=ws))
+    other = d["cache"].clone()
+    step(other, None)  # loads the kernels
+    other.copy_(d["cache"])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(d["cache"], out)
+    for n in range(5):
+        if n > 0:
+            d["lengths"] += 1
+        if n == 3:
+            d["lengths"][1] = 0  # the slot falls idle
+        d["k"].copy_(torch.roll(d["k"], 1, 0) * 1.25)
+        d["v"].copy_(torch.roll(d["v"], 3, 2))
+        d["q"].copy_(torch.roll(d["q"], 1, 1))
+        want = step(other, None)[1]
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(d["cache"], other) and out[0].equal(want[0]) and out[1].equal(want[1]), n
+
+
+def test_other_stream(attt):
+    import torch
+    s = make([300, 20], [2, 2], 4, 2, 91)
+    cache, kh, vh, o, lse = run(attt, s)
+    d = dev(s)
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(st):
+        kh2, vh2 = attt.kv4_append(d["cache"], d["k"], d["v"], d["table"], d["lengths"], row_offsets=s["off"], want_held=True)
+        o2, l2 = attt.kv4_attention(d["q"], d["cache"], d["table"], d["lengths"], row_offsets=s["off"])
+    torch.cuda.current_stream().wait_stream(st)
+    assert np.array_equal(d["cache"].cpu().numpy(), cache) and np.array_equal(host(o2), o) and np.array_equal(host(l2), lse)
+    assert np.array_equal(host(kh2), kh) and np.array_equal(host(vh2), vh)
+
+
+def test_an_episode_from_prompt_to_tokens(attt):
+    """The calls as they run one after the other: prompt attention, its keys and values into the cache, decoding
+    steps with an adapter on the output, and the log-probabilities of the tokens. The attention over the cache is that of
+    the prompt's call on the values the cache holds."""
+    import torch
+    from oracle import logprobs as olp
+    g = torch.Generator("cuda").manual_seed(4)
+    H, kv, d, V = 4, 2, 512, 1000
+    lens = [70, 200]
+    off = np.array([0, 70, 270], np.int64)
+    rand = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16()  # noqa: E731
+    cache = torch.full((8, kv, okv.RECORD), 255, dtype=torch.uint8, device="cuda")
+    table = torch.tensor([[5, 0, 3], [1, 7, 2]], dtype=torch.int32, device="cuda")
+    length = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    q, k, v = rand(270, H, DH), rand(270, kv, DH), rand(270, kv, DH)
+    kh, vh = attt.kv4_append(cache, k, v, table, length, row_offsets=off, want_held=True)
+    o, lse = attt.attention_fwd(q, kh, vh, row_offsets=off)
+    oc, lc = attt.kv4_attention(q, cache, table, length, row_offsets=off)
+    # the same products, the weights rounded to bf16 before and after the scale: twice each output's two roundings
+    assert ((oc.float() - o.float()).abs() <= 2.0 ** -6 * (1.0 + o.float().abs())).all()
+    assert ((lc - lse).abs() <= 1e-5 * (1 + lse.abs())).all()
+    W, A, B = rand(V, d) * 0.05, rand(2, 16, d) * 0.05, rand(2, d, 16) * 0.05
+    held = [(kh[off[e]:off[e + 1]], vh[off[e]:off[e + 1]]) for e in range(2)]
+    for step in range(60):
+        length += 1
+        q1, k1, v1 = rand(2, H, DH), rand(2, kv, DH), rand(2, kv, DH)
+        a, b = attt.kv4_append(cache, k1, v1, table, length, want_held=True)
+        o1, _ = attt.kv4_attention(q1, cache, table, length, max_length=384)
+        held = [(torch.cat([held[e][0], a[e:e + 1]]), torch.cat([held[e][1], b[e:e + 1]])) for e in range(2)]
+        x = o1.view(2, d)
+        y = x.clone()
+        attt.lora_forward([dict(x=x[e:e + 1], y=y[e:e + 1], A=A[e], B=B[e], scale=1.0) for e in range(2)])
+        if step in (0, 57, 59):  # the first sequence passes into its second page at 128
+            for e in range(2):
+                K, Vv = (t.double().cpu().numpy() for t in held[e])
+                for h in range(H):
+                    want, _, mag, _ = okv.attend(q1[e, h].double().cpu().numpy(), K[:, h // 2], Vv[:, h // 2], len(K) - 1, DH ** -0.5)
+                    assert (np.abs(host(o1)[e, h] - want) <= 1.01 * 2.0 ** -8 * (mag + np.abs(want))).all()
+            tokens = torch.tensor([3, 999], dtype=torch.int32, device="cuda")
+            logp, ent, ids, top = attt.token_logprobs(y, W, tokens, top=3)
+            r = olp.token_logprobs(host(y), host(W), tokens.cpu().numpy(), 3)
+            tol = 2.0 ** -23 * (d * r["size"] + V + 32)
+            assert (np.abs(host(logp) - r["logp"]) <= tol).all() and (np.abs(host(ent) - r["entropy"]) <= 16 * tol).all()
+            assert (np.abs(host(top) - r["top"]) <= tol[:, None]).all()

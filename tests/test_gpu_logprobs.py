@@ -1,0 +1,186 @@
+"""Log-probabilities, entropies and alternatives on the GPU against float64.
+
+Hidden states are multiples of 2^-4 and head weights of 2^-9 in most cases, so that every logit is exact in float32 in
+any order of its sums and the alternatives have to agree id by id, ties included. The other outputs' bounds
+count float32 steps: a logit of general values is off by at most d 2^-24 sum |h||w|, an exponential by 2^-22 relative
+with its argument's rounding, the sums by 2^-24 per step (a lane's run, then the joins: at most 2^-24 x 64 in
+all where the runs are added in parallel), lse by the relative error of its sum and one rounding."""
+import numpy as np
+import pytest
+
+from gpu_util import host, note
+from oracle import logprobs as olp
+
+pytestmark = pytest.mark.gpu
+
+
+def grid(N, d, V, seed, lean=True):
+    rng = np.random.default_rng(seed)
+    W = np.round(rng.standard_normal((V, d)) * 0.02 * 512) / 512
+    y = rng.integers(0, V, N).astype(np.int32)
+    h = rng.standard_normal((N, d))
+    if lean:
+        h[::2] += 8.0 * W[y[::2]]
+    return np.clip(np.round(h * 16) / 16, -7.9375, 7.9375), W, y
+
+
+def dev(h, W, y, bf16):
+    import torch
+    dt = torch.bfloat16 if bf16 else torch.float32
+    f = lambda x: torch.from_numpy(np.ascontiguousarray(x, np.float32)).to("cuda", dt)  # noqa: E731
+    return f(h), f(W), torch.from_numpy(y).cuda()
+
+
+def compare(got, r, d, exact, top):
+    logp, ent, ids, lp = got
+    fine = np.isfinite(r["entropy"])
+    # the logit, m - z and lse to 2^-24 of their sizes each; exponentials and sums 2^-18 relative in all
+    span = np.nan_to_num(r["size"]) * (0 if exact else d) + 4 * np.abs(np.nan_to_num(r["logp"])) + 4 * r["size"].clip(0, 256)
+    tol = 2.0 ** -24 * span + 2.0 ** -18
+    for name, x, want in (("logp", host(logp), r["logp"]), ("entropy", host(ent), r["entropy"])):
+        assert np.array_equal(np.isnan(x), np.isnan(want)), name
+        f = ~np.isnan(want)
+        bound = (tol if name == "logp" else 16 * tol)[f]  # an entropy weighs terms of up to 16 of these
+        if f.any():
+            note(f"{name}: largest error over its bound {float((np.abs(x - want)[f] / bound).max()):.3f}")
+        assert (np.abs(x - want)[f] <= bound).all(), name
+    if top == 0:
+        assert ids is None and lp is None
+        return
+    ids, lp = host(ids), host(lp)
+    assert (ids[~fine] == -1).all() and np.isnan(lp[~fine]).all()
+    if exact:
+        assert np.array_equal(ids, r["ids"])
+    assert (np.abs(lp - r["top"])[fine] <= tol[fine, None]).all()
+
+
+CASES = [(1, 8, 1, 1), (1, 64, 5, 5), (3, 72, 300, 7), (17, 128, 4096, 8), (33, 256, 4097, 20), (64, 64, 1000, 32),
+         (129, 136, 2051, 1), (300, 64, 513, 3), (513, 256, 8192, 0), (40, 512, 20001, 8), (700, 128, 3001, 20)]
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("N,d,V,top", CASES)
+def test_rows(attt, N, d, V, top, bf16):
+    note(f"logprobs: N {N}, d {d}, V {V}, top {top}, {'bf16' if bf16 else 'f32'}")
+    h, W, y = grid(N, d, V, N + V)
+    got = attt.token_logprobs(*dev(h, W, y, bf16), top=top)
+    compare(got, olp.token_logprobs(h, W, y, top), d, True, top)
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+def test_general_values(attt, bf16):
+    import torch
+    rng = np.random.default_rng(2)
+    h, W = rng.standard_normal((50, 320)), rng.standard_normal((3000, 320)) * 0.1
+    if bf16:
+        h, W = (torch.from_numpy(x).bfloat16().double().numpy() for x in (h, W))
+    else:
+        h, W = (np.float64(np.float32(x)) for x in (h, W))
+    y = rng.integers(0, 3000, 50).astype(np.int32)
+    compare(attt.token_logprobs(*dev(h, W, y, bf16), top=8), olp.token_logprobs(h, W, y, 8), 320, False, 8)
+
+
+@pytest.mark.parametrize("N", [5, 200])
+@pytest.mark.parametrize("bf16", [True, False])
+def test_ties_take_the_lowest_ids(attt, N, bf16):
+    """Many equal logits: blocks of equal head rows far apart, and rows that are all zero."""
+    h, W, y = grid(N, 64, 9000, 5, lean=False)
+    W[100:9000] = W[np.arange(100, 9000) % 50]
+    h[1] = 0.0
+    r = olp.token_logprobs(h, W, y, 20)
+    assert (r["ids"][1] == np.arange(20)).all()
+    compare(attt.token_logprobs(*dev(h, W, y, bf16), top=20), r, 64, True, 20)
+
+
+@pytest.mark.parametrize("N", [7, 150])
+@pytest.mark.parametrize("bf16", [True, False])
+def test_sorted_heads(attt, N, bf16):
+    """Logits that grow, and that fall, along the vocabulary: every tile replaces the alternatives, or none does."""
+    V, d = 6000, 64
+    W = np.zeros((V, d))
+    W[:, 0] = np.arange(V) // 32 / 512.0
+    W[:, 1] = np.arange(V) % 32 / 512.0
+    h = np.zeros((N, d))
+    h[:, 0], h[:, 1] = 4.0, 0.125
+    h[1::2] *= -1.0
+    if bf16:  # 8 bits hold the first 188 steps
+        W[:, 0] = np.minimum(W[:, 0], 187 / 512.0)
+    y = np.arange(N).astype(np.int32)
+    compare(attt.token_logprobs(*dev(h, W, y, bf16), top=16), olp.token_logprobs(h, W, y, 16), d, True, 16)
+
+
+@pytest.mark.parametrize("N", [6, 140])
+@pytest.mark.parametrize("bf16", [True, False])
+def test_labels_and_values_out_of_range(attt, N, bf16):
+    """Labels outside the vocabulary; NaN and infinities in hidden states, alone in their rows' results."""
+    h, W, y = grid(N, 64, 777, 11)
+    y[0], y[1] = -1, 777
+    h[2, 3], h[3, 3], h[4, 3] = np.nan, np.inf, -np.inf
+    W[:, 3] = 1.0 / 512
+    W[5:700, 3] = 0.5
+    r = olp.token_logprobs(h, W, y, 6)
+    assert np.isnan(r["entropy"][2:5]).all() and np.isfinite(r["entropy"][[0, 1, 5]]).all()
+    compare(attt.token_logprobs(*dev(h, W, y, bf16), top=6), r, 64, True, 6)
+
+
+@pytest.mark.parametrize("N", [3, 130])
+def test_some_logits_of_minus_infinity(attt, N):
+    """Float32 heads whose products overflow to -inf: no weight, and last among the alternatives."""
+    h, W, y = grid(N, 64, 300, 13, lean=False)
+    W[10:290, 0] = -3e38
+    h[:, 0] = 4.0
+    y[0] = 20
+    with np.errstate(over="ignore"):
+        z = (np.float32(h[:, :1]) * np.float32(W[:, 0])).astype(np.float32)
+    assert np.isneginf(z[:, 10:290]).all()
+    t = dev(h, W, y, False)
+    logp, ent, ids, lp = attt.token_logprobs(*t, top=25)
+    keep = np.r_[0:10, 290:300]
+    r = olp.token_logprobs(h, W[keep], np.zeros(N, np.int32), 20)
+    assert np.array_equal(host(ids)[:, :20], keep[r["ids"]]) and np.array_equal(host(ids)[:, 20:], np.tile(np.arange(10, 15), (N, 1)))
+    assert (np.abs(host(lp)[:, :20] - r["top"]) <= 2.0 ** -18).all() and np.isneginf(host(lp)[:, 20:]).all()
+    assert (np.abs(host(ent) - r["entropy"]) <= 2.0 ** -14).all() and np.isneginf(host(logp)[0])
+
+
+def test_outputs_given_repeats_streams_and_graphs(attt):
+    import torch
+    for N, bf16 in ((16, True), (200, True), (70, False)):
+        h, W, y = dev(*grid(N, 128, 3000, 17), bf16)
+        want = attt.token_logprobs(h, W, y, top=5)
+        out = (torch.empty(N, device="cuda"), None, torch.empty(N, 5, dtype=torch.int32, device="cuda"), torch.empty(N, 5, device="cuda"))
+        ws = torch.empty(attt.logprobs_workspace_size(N, 128, 3000, attt.BF16 if bf16 else attt.F32, 5), dtype=torch.uint8, device="cuda")
+        ws.fill_(0xA5)  # its contents are not read
+        st = torch.cuda.Stream()
+        st.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(st):
+            got = attt.token_logprobs(h, W, y, top=5, out=out, workspace=ws)
+        torch.cuda.current_stream().wait_stream(st)
+        assert got[0] is not None and got[1] is None
+        assert all(a.equal(b) for a, b in zip((got[0], got[2], got[3]), (want[0], want[2], want[3])))
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            attt.token_logprobs(h, W, y, top=5, out=out, workspace=ws)
+        for n in range(3):
+            h.copy_(torch.roll(h, 1, 0))
+            want = attt.token_logprobs(h, W, y, top=5)
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(a.equal(b) for a, b in zip((out[0], out[2], out[3]), (want[0], want[2], want[3]))), (N, n)
+
+
+def test_row_chunks(attt):
+    """More rows than are staged at a time: V of 200000 lets 256 MiB hold 335."""
+    import torch
+    g = torch.Generator("cuda").manual_seed(1)
+    N, d, V = 700, 8, 200000
+    h = (torch.randint(-32, 33, (N, d), generator=g, device="cuda") / 16).float()
+    W = (torch.randint(-64, 65, (V, d), generator=g, device="cuda") / 512).float()
+    y = torch.randint(0, V, (N,), generator=g, device="cuda", dtype=torch.int32)
+    logp, ent, ids, lp = attt.token_logprobs(h, W, y, top=4)
+    z = h.double() @ W.double().t()
+    ref = torch.log_softmax(z, 1)
+    assert (logp - ref.gather(1, y.long()[:, None])[:, 0]).abs().max() < 2.0 ** -17
+    best = torch.argsort(z, dim=1, descending=True, stable=True)[:, :4]
+    assert torch.equal(ids.long(), best)
+    assert (lp - ref.gather(1, best)).abs().max() < 2.0 ** -17
