@@ -8,26 +8,32 @@
 
 namespace attt {
 
+constexpr int kFwdTile = BLK * DH * 2, kFwdBuf = 2 * kFwdTile;
+
 // The bits 15 and 31 of the halves of x that hold an infinity or a NaN (exponent bits all set).
 __device__ __forceinline__ uint32_t nonfinite_halves(uint32_t x) { return ((x & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }
 
-// Whether a [64][128] tile holds one: this lane's sixteen 16-byte pieces of it.
-__device__ __forceinline__ bool any_nonfinite(const bf16_t* R, int lane) {
+// Replaces the infinities and NaNs of x by zeros; whether there was one.
+__device__ __forceinline__ bool take_nonfinite(u32x4& x) {
   uint32_t odd = 0;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const u32x4 x = *reinterpret_cast<const u32x4*>(R + (4 * i + (lane >> 4)) * PR + 8 * (lane & 15));
-#pragma unroll
-    for (int e = 0; e < 4; ++e) odd |= nonfinite_halves(x[e]);
-  }
-  return odd != 0;
-}
-
-__device__ __forceinline__ bf16x8 without_nonfinite(bf16x8 f) {
-  u32x4 x = __builtin_bit_cast(u32x4, f);
+  for (int e = 0; e < 4; ++e) odd |= nonfinite_halves(x[e]);
+  if (odd == 0) return false;
 #pragma unroll
   for (int e = 0; e < 4; ++e) x[e] &= ~((nonfinite_halves(x[e]) >> 15) * 0xFFFFu);
-  return __builtin_bit_cast(bf16x8, x);
+  return true;
+}
+
+// trfrag for a tile of swizzled rows of 256 bytes: column 16 j + l16 at rows 32 u + 4 q4 .. +3 and 16 further.
+__device__ __forceinline__ bf16x8 swizzled_trfrag(const uint8_t* R, int j, int u, int lane) {
+  typedef short v4s __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) v4s* lds_v4s;
+  const int r16 = lane >> 2, c = lane & 3;  // row 4 q4 + e of 16; columns 4 c .. +3
+  const uint8_t* p = R + (32 * u + r16) * 256 + (((2 * j + (c >> 1)) ^ r16) << 4) + (c & 1) * 8;
+  const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(p));
+  const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(p + 16 * 256));
+  const uint2 x = __builtin_bit_cast(uint2, lo), y = __builtin_bit_cast(uint2, hi);
+  return __builtin_bit_cast(bf16x8, u32x4{x.x, x.y, y.x, y.y});
 }
 
 // O and lse of one (query head, 64 QT-query block). Wave w owns queries 16 QT w .. + 16 QT - 1 as QT tiles of
@@ -41,12 +47,15 @@ __device__ __forceinline__ bf16x8 without_nonfinite(bf16x8 f) {
 template <int QT>
 __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a, AttnBatch b) {
   constexpr int QBLK = 64 * QT;
-  int ei, h, qb;
-  attn_locate(b, a.heads, true, ei, h, qb);
+  int ei, slot, qb;
+  attn_locate(b, a.heads, true, ei, slot, qb);
   const AttnEp E = b.e[ei];
+  // Workgroups go round the 8 XCDs: eight neighbouring ones take heads far apart, so that an XCD's L2
+  // serves the heads of few key/value heads.
+  const int h = a.heads % 8 == 0 ? slot % 8 * (a.heads / 8) + slot / 8 : slot;
   const int kh = h / (a.heads / a.kv_heads);
   const int q0 = qb * QBLK, nq = min(QBLK, E.L - q0);
-  extern __shared__ __align__(16) uint8_t smem[];  // two buffers of [K tile][V tile], [64][PR] each
+  extern __shared__ __align__(16) uint8_t smem[];  // two buffers of [K tile][V tile], then found[2]
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, q4 = lane >> 4;
   const int64_t qs = (int64_t)a.heads * DH, ks = (int64_t)a.kv_heads * DH;
@@ -63,26 +72,57 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a, AttnBatch 
 #pragma unroll
     for (int j = 0; j < 8; ++j) o[c][j] = f32x4{0, 0, 0, 0};
   }
-  u32x4 fk[4], fv[4];
-  auto fetch = [&](int kb) {
-    const int k0 = kb * BLK, nk = min(BLK, E.L - k0);
-    fetch_block(fk, a.k + ((int64_t)(E.row0 + k0) * a.kv_heads + kh) * DH, ks, nk, tid);
-    fetch_block(fv, a.v + ((int64_t)(E.row0 + k0) * a.kv_heads + kh) * DH, ks, nk, tid);
-  };
   const int kb_last = (q0 + nq - 1) / BLK;  // the key block of the block's last query
+  const int kb_mask = q0 / BLK;             // blocks from here on are hidden from some queries
   const int wq0 = q0 + 16 * QT * w;         // this wave's first query
-  fetch(0);
-  store_block(fk, kv_tile(smem, 0, 0), tid);
-  store_block(fv, kv_tile(smem, 0, 1), tid);
+  // A tile is [64 rows][16 chunks of 16 bytes], chunk c of row r at place c ^ (r % 16): the reads of 16 rows
+  // at one chunk, and the transposing reads of two chunks, fall into all banks. Four rows are one load that goes
+  // to LDS without registers; rows past the episode read as zero.
+  const int drow = 4 * w + (lane >> 4), dchunk = (lane & 15) ^ (drow & 15);
+  const uint32_t doff = (uint32_t)(drow * ks * 2) + dchunk * 16, dstep = (uint32_t)(16 * ks * 2);
+  auto load = [&](int kb) {
+    const int k0 = kb * BLK, nk = min(BLK, E.L - k0);
+    const int64_t at = ((int64_t)(E.row0 + k0) * a.kv_heads + kh) * DH;
+    const int bytes = (int)(((int64_t)(nk - 1) * ks + DH) * 2);
+    const __amdgpu_buffer_rsrc_t rk = buffer_rsrc(a.k + at, bytes), rv = buffer_rsrc(a.v + at, bytes);
+    uint8_t* dst = smem + (kb & 1) * kFwdBuf + w * 1024;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (__attribute__((address_space(3))) void*)(dst + i * 4096), 16,
+                                               doff + i * dstep, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (__attribute__((address_space(3))) void*)(dst + kFwdTile + i * 4096), 16,
+                                               doff + i * dstep, 0, 0, 0);
+    }
+  };
+  // Where some queries do not see all keys of a block, a weight of 0 does not hide an infinity or a NaN in V from the
+  // product. Such entries are taken out of the tile, and the block's number in found[] says that there were some.
+  int* found = reinterpret_cast<int*>(smem + 2 * kFwdBuf);
+  if (tid < 2) found[tid] = -1;
+  load(0);
   for (int kb = 0; kb <= kb_last; ++kb) {
     const int k0 = kb * BLK;
-    // This block's tiles are stored, and every wave is done with the other buffer.
+    // This wave's loads have landed; then every wave's have, and every wave is done with the other buffer.
+    __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
-    if (kb < kb_last) fetch(kb + 1);  // the next key block loads while this one computes
+    if (kb < kb_last) load(kb + 1);  // the next key block loads while this one computes
+    uint8_t* Ks = smem + (kb & 1) * kFwdBuf;
+    uint8_t* Vs = Ks + kFwdTile;
+    if (kb >= kb_mask) {
+      int id = tid;
+      asm volatile("" : "+v"(id));  // its addresses are not kept across the loop
+#pragma unroll 1
+      for (int i = 0; i < 4; ++i) {
+        u32x4* piece = reinterpret_cast<u32x4*>(Vs + (id + 256 * i) * 16);
+        u32x4 x = *piece;
+        if (take_nonfinite(x)) {
+          *piece = x;
+          found[kb & 1] = kb;
+        }
+      }
+      __syncthreads();
+    }
     // A wave whose queries all precede the block has nothing to add.
     if (k0 <= wq0 + 16 * QT - 1) {
-      const bf16_t* Ks = kv_tile(smem, kb & 1, 0);
-      const bf16_t* Vs = kv_tile(smem, kb & 1, 1);
       f32x4 st[QT][4];  // S^T[16 tt + 4 q4 + r][query]
 #pragma unroll
       for (int c = 0; c < QT; ++c)
@@ -93,7 +133,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a, AttnBatch 
 #pragma unroll
         for (int tt = 0; tt < 4; ++tt) {
           const bf16x8 ak = __builtin_bit_cast(
-              bf16x8, *reinterpret_cast<const u32x4*>(Ks + (16 * tt + l16) * PR + 32 * s4 + 8 * q4));
+              bf16x8, *reinterpret_cast<const u32x4*>(Ks + (16 * tt + l16) * 256 + (((4 * s4 + q4) ^ l16) << 4)));
 #pragma unroll
           for (int c = 0; c < QT; ++c) st[c][tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ak, qf[c][s4], st[c][tt], 0, 0, 0);
         }
@@ -107,14 +147,13 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a, AttnBatch 
           for (int tt = 0; tt < 4; ++tt)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              float v = st[c][tt][r] * sl;
               // keys past the episode come after every query of it
-              if constexpr (decltype(masked)::value) v = k0 + 16 * tt + 4 * q4 + r <= wq0 + 16 * c + l16 ? v : -INFINITY;
-              st[c][tt][r] = v;
-              mx = fmaxf(mx, v);
+              if constexpr (decltype(masked)::value)
+                st[c][tt][r] = k0 + 16 * tt + 4 * q4 + r <= wq0 + 16 * c + l16 ? st[c][tt][r] : -INFINITY;
+              mx = fmaxf(mx, st[c][tt][r]);
             }
           mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-          mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+          mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * sl;
           if (__any(mx > m[c] + 8.0f)) {
             const float mn = mx > m[c] + 8.0f ? mx : m[c];  // per row: no other row of the tile changes it
             const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[c] - mn);
@@ -129,7 +168,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a, AttnBatch 
           for (int tt = 0; tt < 4; ++tt)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              st[c][tt][r] = __builtin_amdgcn_exp2f(st[c][tt][r] - ms);
+              st[c][tt][r] = __builtin_amdgcn_exp2f(fmaf(st[c][tt][r], sl, -ms));
               sum += st[c][tt][r];
             }
           l[c] += sum;
@@ -141,47 +180,38 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a, AttnBatch 
                                                        pack_bf16x2(st[c][2 * u + 1][2], st[c][2 * u + 1][3])});
         }
       };
-      const bool whole = k0 + BLK - 1 <= wq0;
-      if (whole)
+      if (k0 + BLK - 1 <= wq0)
         softmax(std::false_type{});
       else
         softmax(std::true_type{});
-      auto product = [&](auto clean) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+      for (int j = 0; j < 8; ++j)
 #pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            bf16x8 av = trfrag(Vs, 16 * j, u, lane);
-            if constexpr (decltype(clean)::value) av = without_nonfinite(av);
+        for (int u = 0; u < 2; ++u) {
+          const bf16x8 av = swizzled_trfrag(Vs, j, u, lane);
 #pragma unroll
-            for (int c = 0; c < QT; ++c) o[c][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, p[c][u], o[c][j], 0, 0, 0);
-          }
-      };
-      // Where some queries do not see all keys, a weight of 0 does not hide an infinity or a NaN in V from the
-      // product. Such entries are left out of it and added to the queries that see them.
-      if (!whole && __any(any_nonfinite(Vs, lane))) {
-        product(std::true_type{});
+          for (int c = 0; c < QT; ++c) o[c][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, p[c][u], o[c][j], 0, 0, 0);
+        }
+      if (kb >= kb_mask && found[kb & 1] == kb) {  // the entries taken out, for the queries that see them
+        int id = lane;
+        asm volatile("" : "+v"(id));
+        const bf16_t* vb = a.v + ((int64_t)(E.row0 + k0) * a.kv_heads + kh) * DH + 4 * (id >> 4);
+        const int nk = min(BLK, E.L - k0);
 #pragma unroll 1
-        for (int s = 0; s < BLK; ++s)
+        for (int s = 0; s < nk; ++s)
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            const uint2 x = *reinterpret_cast<const uint2*>(Vs + s * PR + 16 * j + 4 * q4);
+            const uint2 x = *reinterpret_cast<const uint2*>(vb + s * ks + 16 * j);
+            if (!(nonfinite_halves(x.x) | nonfinite_halves(x.y))) continue;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
               const float v = bf16_bits_to_f32((r < 2 ? x.x : x.y) >> (r & 1 ? 16 : 0) & 0xFFFFu);
-              if (__builtin_isfinite(v)) continue;
 #pragma unroll
               for (int c = 0; c < QT; ++c)
-                if (k0 + s <= wq0 + 16 * c + l16) o[c][j][r] += v;
+                if (!__builtin_isfinite(v) && k0 + s <= wq0 + 16 * c + (id & 15)) o[c][j][r] += v;
             }
           }
-      } else {
-        product(std::false_type{});
       }
-    }
-    if (kb < kb_last) {
-      store_block(fk, kv_tile(smem, (kb + 1) & 1, 0), tid);
-      store_block(fv, kv_tile(smem, (kb + 1) & 1, 1), tid);
     }
   }
 #pragma unroll
@@ -220,7 +250,7 @@ __global__ __launch_bounds__(256) void attn_dsum_kernel(AttnArgs a) {
 
 template <int QT>
 static hipError_t launch_fwd(LdsLimit& limit, const AttnArgs& a, AttnBatch b, hipStream_t s) {
-  constexpr size_t lds = 2 * (size_t)kKvBuf;
+  constexpr size_t lds = 2 * (size_t)kFwdBuf + 16;
   if (hipError_t e = limit.raise((const void*)attn_fwd_kernel<QT>, lds)) return e;
   int n = 0;
   for (int i = 0; i < b.count; ++i) {
