@@ -137,6 +137,14 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a, AttnBatch 
 #pragma unroll
           for (int c = 0; c < QT; ++c) st[c][tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ak, qf[c][s4], st[c][tt], 0, 0, 0);
         }
+      // three K fragments stay ahead of their products
+      __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+#pragma unroll
+      for (int n = 0; n < 13; ++n) {
+        __builtin_amdgcn_sched_group_barrier(0x008, QT, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, 3 * QT, 0);
       bf16x8 p[QT][2];  // weights of keys 32 u + 4 q4 .. +3 and 32 u + 16 + 4 q4 .. +3
       // A key block that ends at or before the wave's first query is whole and entirely allowed: no mask there.
       auto softmax = [&](auto masked) {
@@ -152,8 +160,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a, AttnBatch 
                 st[c][tt][r] = k0 + 16 * tt + 4 * q4 + r <= wq0 + 16 * c + l16 ? st[c][tt][r] : -INFINITY;
               mx = fmaxf(mx, st[c][tt][r]);
             }
-          mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-          mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * sl;
+          mx = rows_max(mx) * sl;
           if (__any(mx > m[c] + 8.0f)) {
             const float mn = mx > m[c] + 8.0f ? mx : m[c];  // per row: no other row of the tile changes it
             const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[c] - mn);
@@ -192,6 +199,13 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a, AttnBatch 
 #pragma unroll
           for (int c = 0; c < QT; ++c) o[c][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, p[c][u], o[c][j], 0, 0, 0);
         }
+      // two V fragments stay ahead of their products
+      __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+      for (int n = 0; n < 15; ++n) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, QT, 0);
+      }
       if (kb >= kb_mask && found[kb & 1] == kb) {  // the entries taken out, for the queries that see them
         int id = lane;
         asm volatile("" : "+v"(id));
@@ -217,9 +231,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a, AttnBatch 
 #pragma unroll
   for (int c = 0; c < QT; ++c) {
     const int qry = 16 * QT * w + 16 * c + l16;
-    float lc = l[c];
-    lc += __shfl_xor(lc, 16, 64);
-    lc += __shfl_xor(lc, 32, 64);
+    const float lc = rows_sum(l[c]);
     if (qry < nq) {
       if (q4 == 0) a.lse[(int64_t)h * a.N + E.row0 + q0 + qry] = m[c] / kLog2e + logf(lc);
       const float inv = 1.0f / lc;

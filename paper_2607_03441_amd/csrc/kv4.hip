@@ -274,8 +274,7 @@ __global__ __launch_bounds__(256) void kv4_attention_kernel(Kv4Args a, Kv4Batch 
             st[c][i][r] = v;
             mx = fmaxf(mx, v);
           }
-        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        mx = rows_max(mx);
         if (__any(mx > m[c] + 8.0f)) {
           const float mn = mx > m[c] + 8.0f ? mx : m[c];  // per row: no other row of the tile changes it
           const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[c] - mn);
@@ -328,8 +327,7 @@ __global__ __launch_bounds__(256) void kv4_attention_kernel(Kv4Args a, Kv4Batch 
   float2* ml = reinterpret_cast<float2*>(smem + 2 * (size_t)RT * 8 * 64 * sizeof(f32x4));
 #pragma unroll
   for (int c = 0; c < RT; ++c) {
-    l[c] += __shfl_xor(l[c], 16, 64);
-    l[c] += __shfl_xor(l[c], 32, 64);
+    l[c] = rows_sum(l[c]);
     if (bad) l[c] = __uint_as_float(0x7FC00000u);
   }
 #pragma unroll
