@@ -45,7 +45,7 @@ static const char* kKernelNames[K_NUM_KERNELS] = {
     "ce_loss", "ce_head_transpose", "ce_bwd_dz", "ce_bwd_dh", "ce_overflow_guard", "lora_u_du", "lora_dadb",
     "lora_reduce", "ngram_set", "ngram_set_weight", "lora_sgd", "ce_fused_bwd", "rep_count", "rep_reduce", "attn_fwd_stats",
     "attn_dkdv", "attn_dq", "lora_fwd", "lora_swap", "attn_fwd", "attn_dsum", "kv4_append", "kv4_attention", "kv4_join",
-    "logprob_logits", "logprob_rows", "logprob_join"};
+    "logprob_logits", "logprob_rows", "logprob_join", "logprob_fused"};
 
 const char* kernel_name(int id) { return (id >= 0 && id < K_NUM_KERNELS) ? kKernelNames[id] : nullptr; }
 

@@ -227,9 +227,13 @@ extern "C" attt_status attt_kv4_attention(const void* q, const void* cache, int6
 // ------------------------------------------------------------------------------------------
 namespace {
 
+constexpr int64_t kLpStagedRows = 32;     // bf16: at most so many rows are staged
+constexpr int64_t kLpFusedRows = 65536;   // rows of a launch without staging, which bounds the workspace
+
 struct LpPlan {
-  int64_t ldz = 0, rows = 0;  // staged logits: row length, rows at a time
-  int32_t splits = 0;
+  bool fused = false;          // no staged logits
+  int64_t ldz = 0, rows = 0;   // staged logits: row length; rows at a time
+  int32_t splits = 0, places = 0;
   size_t off_stats = 0, off_lists = 0, total = 0;
 };
 
@@ -245,16 +249,31 @@ attt_status lp_check(int64_t N, int64_t d, int64_t V, int32_t dtype, int32_t top
   return ATTT_OK;
 }
 
-LpPlan lp_plan(int64_t N, int64_t V, int32_t top) {
+LpPlan lp_plan(int64_t N, int64_t V, int32_t dtype, int32_t top) {
   LpPlan P;
-  P.ldz = round_up(V, 64);
-  // rows of about 256 MiB of logits at a time
-  const int64_t fit = ((int64_t)256 << 20) / (P.ldz * 4);
-  P.rows = std::min<int64_t>(std::max<int64_t>(N, 1), fit >= 128 ? fit / 128 * 128 : std::max<int64_t>(1, fit));
-  P.splits = (int32_t)ceil_div(V, kLpRowChunk);
+  P.fused = dtype == ATTT_BF16 && N > kLpStagedRows;
+  if (P.fused) {
+    P.rows = std::min(N, kLpFusedRows);
+    // Row tiles x splits workgroups, one per CU at a time: the splits with the fewest tiles one after the other, a
+    // workgroup's start and end counted as a third of a tile.
+    const int64_t tiles_t = ceil_div(P.rows, 256), tiles_v = ceil_div(V, 256);
+    double best = 0.0;
+    for (int64_t s = 1; s <= std::min<int64_t>(tiles_v, 256); ++s) {
+      const double cost = (double)ceil_div(tiles_t * s, 256) * ((double)ceil_div(tiles_v, s) + 0.3);
+      if (s == 1 || cost < best) best = cost, P.splits = (int32_t)s;
+    }
+    P.places = top <= 8 ? 8 : top <= 16 ? 16 : 32;
+  } else {
+    P.ldz = round_up(V, 64);
+    // rows of about 256 MiB of logits at a time
+    const int64_t fit = ((int64_t)256 << 20) / (P.ldz * 4);
+    P.rows = std::min<int64_t>(std::max<int64_t>(N, 1), fit >= 128 ? fit / 128 * 128 : std::max<int64_t>(1, fit));
+    P.splits = (int32_t)ceil_div(V, kLpRowChunk);
+    P.places = top;
+  }
   P.off_stats = align256((size_t)P.rows * P.ldz * 4);
   P.off_lists = P.off_stats + align256((size_t)P.rows * P.splits * sizeof(float4));
-  P.total = P.off_lists + align256((size_t)P.rows * P.splits * top * sizeof(float2));
+  P.total = P.off_lists + (top > 0 ? align256((size_t)P.rows * P.splits * P.places * sizeof(float2)) : 0);
   return P;
 }
 
@@ -264,7 +283,7 @@ extern "C" attt_status attt_logprobs_workspace_size(int64_t N, int64_t d, int64_
   if (!bytes) return fail(ATTT_EINVAL, "logprobs: bytes is null");
   attt_status st = lp_check(N, d, V, dtype, top);
   if (st) return st;
-  *bytes = lp_plan(N, V, top).total;
+  *bytes = lp_plan(N, V, dtype, top).total;
   return ATTT_OK;
 }
 
@@ -279,7 +298,7 @@ extern "C" attt_status attt_token_logprobs(const void* hidden, const void* lm_he
   if (top > 0 && (!top_ids || !top_logp)) return fail(ATTT_EINVAL, "logprobs: null pointer");
   if (!aligned16(hidden) || !aligned16(lm_head))
     return fail(ATTT_EINVAL, "logprobs: hidden and lm_head must be 16-byte aligned");
-  const LpPlan P = lp_plan(N, V, top);
+  const LpPlan P = lp_plan(N, V, dtype, top);
   if (workspace_bytes < P.total) return fail(ATTT_ENOSPACE, "logprobs: workspace %zu bytes, need %zu", workspace_bytes, P.total);
   if (!workspace) return fail(ATTT_EINVAL, "logprobs: workspace is null");
   if (!aligned256(workspace)) return fail(ATTT_EINVAL, "logprobs: workspace must be 256-byte aligned");
@@ -300,12 +319,17 @@ extern "C" attt_status attt_token_logprobs(const void* hidden, const void* lm_he
   a.V = (int32_t)V;
   a.top = top;
   a.splits = P.splits;
+  a.places = P.places;
   hipStream_t s = static_cast<hipStream_t>(stream);
   for (int64_t r0 = 0; r0 < N; r0 += P.rows) {
     a.row0 = (int32_t)r0;
     a.rows = (int32_t)std::min(P.rows, N - r0);
-    HIP_TRY(launch_lp_logits(dtype, a, s), "logprob_logits");
-    HIP_TRY(launch_lp_rows(a, s), "logprob_rows");
+    if (P.fused) {
+      HIP_TRY(launch_lp_fused(a, s), "logprob_fused");
+    } else {
+      HIP_TRY(launch_lp_logits(dtype, a, s), "logprob_logits");
+      HIP_TRY(launch_lp_rows(a, s), "logprob_rows");
+    }
     HIP_TRY(launch_lp_join(a, s), "logprob_join");
   }
   return ATTT_OK;

@@ -44,6 +44,7 @@ enum KernelId {
   K_LP_LOGITS,
   K_LP_ROWS,
   K_LP_JOIN,
+  K_LP_FUSED,
   K_NUM_KERNELS
 };
 
@@ -238,17 +239,19 @@ struct LpArgs {
   const int32_t* labels; // [N]
   float* logits;         // staged rows [rows][ldz]
   float4* stats;         // [row][split]: maximum m, sum exp(z - m), sum (z - m) exp(z - m), label logit (NaN: not here)
-  float2* lists;         // [row][split][top]: logit, id (as bits; -1: none)
+  float2* lists;         // [row][split][places]: logit, id (as bits; -1: none), the first `top` of them
   float* logp;           // [N]
   float* entropy;        // [N] or null
   int32_t* top_ids;      // [N][top]
   float* top_logp;       // [N][top]
   int64_t ldz;
   int32_t N, d, V, top;
-  int32_t row0, rows;    // the staged rows
-  int32_t splits;
+  int32_t row0, rows;    // the rows of the launch
+  int32_t splits, places;
 };
 hipError_t launch_lp_logits(int dtype, const LpArgs& a, hipStream_t s);
+// bf16: statistics and lists of `splits` parts of the vocabulary, without staged logits; places: 8, 16 or 32
+hipError_t launch_lp_fused(const LpArgs& a, hipStream_t s);
 hipError_t launch_lp_rows(const LpArgs& a, hipStream_t s);
 hipError_t launch_lp_join(const LpArgs& a, hipStream_t s);
 

@@ -19,6 +19,7 @@ struct Cand {
 };
 __device__ __forceinline__ bool better(Cand a, Cand b) { return a.z > b.z || (a.z == b.z && a.id < b.id); }
 constexpr uint32_t kNone = 0xFFFFFFFFu;
+constexpr float kLog2e = 1.4426950408889634f;
 
 __device__ __forceinline__ Cand wave_best(Cand c) {
 #pragma unroll
@@ -127,6 +128,212 @@ __global__ __launch_bounds__(256) void lp_logits_f32_kernel(LpArgs a, int tiles_
   }
 }
 
+// The logits of a row tile of 256 tokens without memory for them: a persistent workgroup walks the vocabulary tiles split,
+// split + splits, ... of the product z^T = W h^T (gemm_core.hpp's 256 x 256 tiles on eight waves) and takes what it
+// needs from each while the next tile's first loads are on their way. A lane holds 32 logits of each of 4 tokens.
+// Statistics: every token's (m, s, t) per half of the tile's rows (wave row), kept in LDS.
+// Alternatives: a token's list of the best so far lies in its place of `lists`, the last of it as a threshold in LDS.
+// A tile's logits above the threshold are handed to the token's thread through kHand places in LDS, in as
+// many rounds as it takes; that thread sorts them into the list and raises the threshold. After the first tile
+// there are few: a tile of M replaces about top / M of them. Ids grow from tile to tile, so that a logit equal to the
+// threshold never displaces an earlier one; within a tile the ids decide. The list does not depend on
+// the order in which candidates arrive.
+constexpr int kHand = 8;
+struct LpFusedLds {
+  float m[2][256], s[2][256], t[2][256];
+  float zy[256];        // the label's logit; NaN until it has been met
+  int32_t y[256];       // the label; negative: none in the vocabulary
+  float thr[256];       // the list's last logit; NaN: the list is not full; +inf: no list
+  uint32_t thr_id[256]; // and its id
+  int32_t count[256];   // candidates of the round, kHand of which have a place
+  Cand hand[256][kHand];
+};
+constexpr size_t kLpFusedLds = CfgBig::LDS + sizeof(LpFusedLds);
+static_assert(kLpFusedLds <= 160 * 1024, "LDS");
+
+// KB: places of a list (0: no alternatives)
+template <int KB>
+__global__ __launch_bounds__(512) void lp_fused_kernel(LpArgs a, int tiles_t, int tiles_v) {
+  using C = CfgBig;
+  extern __shared__ __align__(16) uint8_t smem[];
+  bf16_t* stages = reinterpret_cast<bf16_t*>(smem);
+  LpFusedLds& L = *reinterpret_cast<LpFusedLds*>(smem + C::LDS);
+  const int tid = threadIdx.x;
+  int tt, split;
+  tile_of(blockIdx.x, tiles_t, a.splits, tt, split);
+  const int t0 = tt * 256, nt = min(256, a.rows - t0);
+  if (tid < 256) {
+    L.m[0][tid] = L.m[1][tid] = -INFINITY;
+    L.s[0][tid] = L.s[1][tid] = L.t[0][tid] = L.t[1][tid] = 0.0f;
+    L.zy[tid] = __uint_as_float(0x7FC00000u);
+    const int y = tid < nt ? a.labels[a.row0 + t0 + tid] : -1;
+    L.y[tid] = y < a.V ? y : -1;
+    L.thr[tid] = tid < nt ? __uint_as_float(0x7FC00000u) : INFINITY;
+    L.thr_id[tid] = kNone;
+    L.count[tid] = 0;
+  }
+  const bf16_t* W = static_cast<const bf16_t*>(a.W);
+  const bf16_t* h = static_cast<const bf16_t*>(a.h) + (int64_t)(a.row0 + t0) * a.d;
+  auto prologue = [&](int tv, int id) {
+    mfma_pp_prologue<C>(W + (int64_t)tv * 256 * a.d, a.d, a.V - tv * 256, h, a.d, nt, a.d, stages, id);
+  };
+  prologue(split, tid);
+  bool first = true;
+  for (int tv = split; tv < tiles_v; tv += a.splits, first = false) {
+    int id = tid;
+    asm volatile("" : "+v"(id));  // what is derived from it is not kept across the mainloop
+    const int v0 = tv * 256;
+    Acc16 acc;
+    mfma_mainloop_pp16<C>(W + (int64_t)v0 * a.d, a.d, a.V - v0, h, a.d, nt, a.d, stages, acc, id, true);
+    if (tv + a.splits < tiles_v) prologue(tv + a.splits, id);
+    const int lane = id & 63, w = __builtin_amdgcn_readfirstlane(id >> 6);
+    const int wm = w >> 2, l16 = lane & 15, q4 = lane >> 4;
+    const int vb = v0 + wm * 128 + 4 * q4;  // entry (i, r) of the lane: vb + 16 i + r
+    uint32_t pending[Mma16::TN];            // bit 4 i + r
+    const bool whole = v0 + 256 <= a.V;
+#pragma unroll
+    for (int j = 0; j < Mma16::TN; ++j) {
+      const int tok = (w & 3) * 64 + 16 * j + l16;
+      if (!whole) {
+#pragma unroll
+        for (int i = 0; i < Mma16::TM; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (vb + 16 * i + r >= a.V) acc[i][j][r] = -INFINITY;
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < Mma16::TM; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) mx = fmaxf(mx, acc[i][j][r]);
+      const float m_old = L.m[wm][tok], m = fmaxf(m_old, rows_max(mx));
+      const float m0 = m == -INFINITY ? 0.0f : m;
+      const float mb = m0 * kLog2e;
+      float s = 0.0f, t = 0.0f;
+#pragma unroll
+      for (int i = 0; i < Mma16::TM; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float e = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], kLog2e, -mb));
+          s += e;
+          t = fmaf(fmaxf(acc[i][j][r] - m0, -200.0f), e, t);  // e is 0 there: -inf times it would not be
+        }
+      s = rows_sum(s);
+      t = rows_sum(t);
+      const float s_old = L.s[wm][tok], t_old = L.t[wm][tok];
+      const float dm = m_old == -INFINITY ? 0.0f : m_old - m0, f = __builtin_amdgcn_exp2f(dm * kLog2e);
+      const int y = L.y[tok] - (v0 + wm * 128);
+      const bool has = y >= 0 && y < 128 && (y >> 2 & 3) == q4;
+      if (__any(has)) {
+        const int e = (y >> 4) * 4 + (y & 3);
+        float z = 0.0f;
+#pragma unroll
+        for (int i = 0; i < Mma16::TM; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (e == 4 * i + r) z = acc[i][j][r];
+        if (has) L.zy[tok] = z;
+      }
+      // all of the wave's reads of the token's old values come before the writes
+      if (q4 == 0) {
+        L.m[wm][tok] = m;
+        L.s[wm][tok] = s_old * f + s;
+        L.t[wm][tok] = (t_old + dm * s_old) * f + t;
+      }
+      if constexpr (KB > 0) {
+        const float thr = L.thr[tok];
+        uint32_t p = 0;
+#pragma unroll
+        for (int i = 0; i < Mma16::TM; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (!(acc[i][j][r] <= thr) && (whole || vb + 16 * i + r < a.V)) p |= 1u << (4 * i + r);
+        pending[j] = p;
+      }
+    }
+    if constexpr (KB > 0) {
+      for (;;) {
+#pragma unroll
+        for (int j = 0; j < Mma16::TN; ++j) {
+          const int tok = (w & 3) * 64 + 16 * j + l16;
+          if (pending[j]) {
+#pragma unroll
+            for (int i = 0; i < Mma16::TM; ++i)
+#pragma unroll
+              for (int r = 0; r < 4; ++r)
+                if (pending[j] >> (4 * i + r) & 1) {
+                  const int at = atomicAdd(&L.count[tok], 1);
+                  if (at < kHand) {
+                    L.hand[tok][at] = {acc[i][j][r], (uint32_t)(vb + 16 * i + r)};
+                    pending[j] &= ~(1u << (4 * i + r));
+                  }
+                }
+          }
+        }
+        __syncthreads();
+        bool more = false;
+        const int n = id < 256 ? L.count[id] : 0;
+        if (n > 0) {
+          more = n > kHand;
+          Cand list[KB];
+          float2* mine = a.lists + ((int64_t)(t0 + id) * a.splits + split) * KB;
+          const bool fresh = first && L.thr_id[id] == kNone;  // nothing has been written yet
+#pragma unroll
+          for (int k = 0; k < KB; ++k) {
+            const float2 x = fresh ? make_float2(-INFINITY, __uint_as_float(kNone)) : mine[k];
+            list[k] = {x.x, __float_as_uint(x.y)};
+          }
+          bool nan = false;
+#pragma unroll 1
+          for (int c = 0; c < min(n, kHand); ++c) {
+            Cand x = L.hand[id][c];
+            nan |= x.z != x.z;
+#pragma unroll
+            for (int k = 0; k < KB; ++k) {
+              const bool up = better(x, list[k]);
+              const Cand y = up ? list[k] : x;
+              list[k] = up ? x : list[k];
+              x = y;
+            }
+          }
+          Cand last = list[0];
+#pragma unroll
+          for (int k = 0; k < KB; ++k) {
+            mine[k] = make_float2(list[k].z, __uint_as_float(list[k].id));
+            if (k == a.top - 1) last = list[k];
+          }
+          // an id marks the list as written even while it is not full
+          L.thr[id] = nan ? INFINITY : last.id == kNone ? __uint_as_float(0x7FC00000u) : last.z;
+          L.thr_id[id] = last.id == kNone ? kNone - 1 : last.id;
+          L.count[id] = 0;
+        }
+        if (!__syncthreads_or(more)) break;
+#pragma unroll
+        for (int j = 0; j < Mma16::TN; ++j) {
+          const int tok = (w & 3) * 64 + 16 * j + l16;
+          const float thr = L.thr[tok];
+          const uint32_t ti = L.thr_id[tok];
+#pragma unroll
+          for (int i = 0; i < Mma16::TM; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (acc[i][j][r] < thr || (acc[i][j][r] == thr && (uint32_t)(vb + 16 * i + r) > ti)) pending[j] &= ~(1u << (4 * i + r));
+        }
+      }
+    }
+  }
+  __syncthreads();
+  if (tid < nt) {
+    float m = L.m[0][tid], s = L.s[0][tid], t = L.t[0][tid];
+    stats_join(m, s, t, L.m[1][tid], L.s[1][tid], L.t[1][tid]);
+    const int64_t at = (int64_t)(t0 + tid) * a.splits + split;
+    a.stats[at] = make_float4(m, s, t, L.zy[tid]);
+    if constexpr (KB > 0)
+      if (L.thr_id[tid] == kNone)  // not one candidate
+        for (int k = 0; k < KB; ++k) a.lists[at * KB + k] = make_float2(-INFINITY, __uint_as_float(kNone));
+  }
+}
+
 // Statistics and the best `top` of kLpRowChunk logits of one staged row: 16 a thread, in registers. The best
 // are drawn one after the other: the best of each thread's, of each wave's, of the workgroup's.
 __global__ __launch_bounds__(256) void lp_rows_kernel(LpArgs a) {
@@ -188,7 +395,7 @@ __global__ __launch_bounds__(256) void lp_rows_kernel(LpArgs a) {
 #pragma unroll
     for (int i = 1; i < 4; ++i)
       if (better(best[n & 1][i], b)) b = best[n & 1][i];
-    if (tid == 0) a.lists[at * a.top + n] = make_float2(b.z, __uint_as_float(b.id));
+    if (tid == 0) a.lists[at * a.places + n] = make_float2(b.z, __uint_as_float(b.id));
     if (b.id != kNone && b.id == c.id) {
       const int rel = (int)b.id - v0;
       taken |= 1u << (rel / 1024 * 4 + (rel & 3));
@@ -226,7 +433,7 @@ __global__ __launch_bounds__(256) void lp_join_kernel(LpArgs a) {
   for (int k = 0; k < a.top; ++k) {
     Cand c = {-INFINITY, kNone};
     for (int i = lane; i < n; i += 64) {
-      const float2 x = a.lists[at * a.top + i];
+      const float2 x = a.lists[(at + i / a.top) * a.places + i % a.top];
       const Cand y = {x.x, __float_as_uint(x.y)};
       if (y.id != kNone && (first || better(last, y)) && better(y, c)) c = y;
     }
@@ -253,6 +460,20 @@ hipError_t launch_lp_logits(int dtype, const LpArgs& a, hipStream_t s) {
     hipLaunchKernelGGL(lp_logits_f32_kernel, dim3(tv * tt), dim3(256), 0, s, a, tt);
   }
   return hipGetLastError();
+}
+
+template <int KB>
+static hipError_t launch_fused(const LpArgs& a, hipStream_t s) {
+  static LdsLimit limit;
+  if (hipError_t e = limit.raise((const void*)lp_fused_kernel<KB>, kLpFusedLds)) return e;
+  const int tiles_t = (a.rows + 255) / 256, tiles_v = (a.V + 255) / 256;
+  KernelTimer t(K_LP_FUSED, s);
+  hipLaunchKernelGGL(lp_fused_kernel<KB>, dim3(tiles_t * a.splits), dim3(512), kLpFusedLds, s, a, tiles_t, tiles_v);
+  return hipGetLastError();
+}
+
+hipError_t launch_lp_fused(const LpArgs& a, hipStream_t s) {
+  return a.top == 0 ? launch_fused<0>(a, s) : a.places == 8 ? launch_fused<8>(a, s) : a.places == 16 ? launch_fused<16>(a, s) : launch_fused<32>(a, s);
 }
 
 hipError_t launch_lp_rows(const LpArgs& a, hipStream_t s) {
