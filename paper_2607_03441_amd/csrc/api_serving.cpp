@@ -227,13 +227,12 @@ extern "C" attt_status attt_kv4_attention(const void* q, const void* cache, int6
 // ------------------------------------------------------------------------------------------
 namespace {
 
-constexpr int64_t kLpStagedRows = 32;     // bf16: at most so many rows are staged
 constexpr int64_t kLpFusedRows = 65536;   // rows of a launch without staging, which bounds the workspace
 
 struct LpPlan {
   bool fused = false;          // no staged logits
   int64_t ldz = 0, rows = 0;   // staged logits: row length; rows at a time
-  int32_t splits = 0, places = 0;
+  int32_t splits = 0, block = 0;
   size_t off_stats = 0, off_lists = 0, total = 0;
 };
 
@@ -251,7 +250,7 @@ attt_status lp_check(int64_t N, int64_t d, int64_t V, int32_t dtype, int32_t top
 
 LpPlan lp_plan(int64_t N, int64_t V, int32_t dtype, int32_t top) {
   LpPlan P;
-  P.fused = dtype == ATTT_BF16 && N > kLpStagedRows;
+  P.fused = dtype == ATTT_BF16 && top <= kLpFusedTop && N > 128 && (top == 0 || N * V >= 10000000);
   if (P.fused) {
     P.rows = std::min(N, kLpFusedRows);
     // Row tiles x splits workgroups, one per CU at a time: the splits with the fewest tiles one after the other, a
@@ -262,18 +261,18 @@ LpPlan lp_plan(int64_t N, int64_t V, int32_t dtype, int32_t top) {
       const double cost = (double)ceil_div(tiles_t * s, 256) * ((double)ceil_div(tiles_v, s) + 0.3);
       if (s == 1 || cost < best) best = cost, P.splits = (int32_t)s;
     }
-    P.places = top <= 8 ? 8 : top <= 16 ? 16 : 32;
+    P.block = 256;
   } else {
     P.ldz = round_up(V, 64);
     // rows of about 256 MiB of logits at a time
     const int64_t fit = ((int64_t)256 << 20) / (P.ldz * 4);
     P.rows = std::min<int64_t>(std::max<int64_t>(N, 1), fit >= 128 ? fit / 128 * 128 : std::max<int64_t>(1, fit));
     P.splits = (int32_t)ceil_div(V, kLpRowChunk);
-    P.places = top;
+    P.block = (int32_t)P.rows;
   }
   P.off_stats = align256((size_t)P.rows * P.ldz * 4);
   P.off_lists = P.off_stats + align256((size_t)P.rows * P.splits * sizeof(float4));
-  P.total = P.off_lists + (top > 0 ? align256((size_t)P.rows * P.splits * P.places * sizeof(float2)) : 0);
+  P.total = P.off_lists + (top > 0 ? align256((size_t)round_up(P.rows, P.block) * P.splits * top * sizeof(float2)) : 0);
   return P;
 }
 
@@ -319,7 +318,7 @@ extern "C" attt_status attt_token_logprobs(const void* hidden, const void* lm_he
   a.V = (int32_t)V;
   a.top = top;
   a.splits = P.splits;
-  a.places = P.places;
+  a.block = P.block;
   hipStream_t s = static_cast<hipStream_t>(stream);
   for (int64_t r0 = 0; r0 < N; r0 += P.rows) {
     a.row0 = (int32_t)r0;

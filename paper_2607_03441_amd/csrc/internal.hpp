@@ -232,14 +232,15 @@ hipError_t launch_kv4_attention(int row_tiles, const Kv4Args& a, const Kv4Batch&
 
 // ---- log-probabilities of given tokens -------------------------------------------------------------
 constexpr int kLpMaxTop = 32;       // most alternatives
+constexpr int kLpFusedTop = 10;      // most alternatives that have a place in LDS beside the product's tiles
 constexpr int kLpRowChunk = 4096;   // logits a workgroup of the row kernel takes
 struct LpArgs {
   const void* h;         // [N][d]
   const void* W;         // [V][d]
   const int32_t* labels; // [N]
   float* logits;         // staged rows [rows][ldz]
-  float4* stats;         // [row][split]: maximum m, sum exp(z - m), sum (z - m) exp(z - m), label logit (NaN: not here)
-  float2* lists;         // [row][split][places]: logit, id (as bits; -1: none), the first `top` of them
+  float4* stats;         // [split][row]: maximum m, sum exp(z - m), sum (z - m) exp(z - m), label logit (NaN: not here)
+  float2* lists;         // [split][block of rows][top][row of the block]: logit, id (as bits; -1: none)
   float* logp;           // [N]
   float* entropy;        // [N] or null
   int32_t* top_ids;      // [N][top]
@@ -247,10 +248,10 @@ struct LpArgs {
   int64_t ldz;
   int32_t N, d, V, top;
   int32_t row0, rows;    // the rows of the launch
-  int32_t splits, places;
+  int32_t splits, block;
 };
 hipError_t launch_lp_logits(int dtype, const LpArgs& a, hipStream_t s);
-// bf16: statistics and lists of `splits` parts of the vocabulary, without staged logits; places: 8, 16 or 32
+// bf16, top <= kLpFusedTop: statistics and lists of `splits` parts of the vocabulary, without staged logits
 hipError_t launch_lp_fused(const LpArgs& a, hipStream_t s);
 hipError_t launch_lp_rows(const LpArgs& a, hipStream_t s);
 hipError_t launch_lp_join(const LpArgs& a, hipStream_t s);

@@ -4,6 +4,8 @@
 //   the `top` largest z_v - lse with their ids, equal logits in the order of their ids.
 // With m any reference, s = sum exp(z - m) and t = sum (z - m) exp(z - m): lse = m + log s and
 // entropy = log s - t / s, which does not cancel where one token has nearly all the probability.
+#include <type_traits>
+
 #include "common.hpp"
 #include "gemm_core.hpp"
 #include "internal.hpp"
@@ -21,13 +23,36 @@ __device__ __forceinline__ bool better(Cand a, Cand b) { return a.z > b.z || (a.
 constexpr uint32_t kNone = 0xFFFFFFFFu;
 constexpr float kLog2e = 1.4426950408889634f;
 
+// The best of a wave's candidates: the largest logit, then the lowest id that has it, both by exchanges within
+// rows of 16 lanes and swaps between rows (shuffles through LDS took five times as long).
+template <class T, class Op>
+__device__ __forceinline__ T wave_reduce(T v, Op op) {
+  static_assert(sizeof(T) == 4, "32-bit lanes");
+  auto step = [&](auto ctrl) {
+    v = op(v, __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(ctrl)::value, 0xF, 0xF, false)));
+  };
+  step(std::integral_constant<int, 0xB1>{});   // lanes 1, 0, 3, 2 of four
+  step(std::integral_constant<int, 0x4E>{});   // lanes 2, 3, 0, 1
+  step(std::integral_constant<int, 0x141>{});  // mirrored half rows
+  step(std::integral_constant<int, 0x140>{});  // mirrored rows
+  const uint32_t x = __builtin_bit_cast(uint32_t, v);
+  const auto p = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  const uint32_t p0 = p[0], p1 = p[1];
+  const uint32_t y = __builtin_bit_cast(uint32_t, op(__builtin_bit_cast(T, p0), __builtin_bit_cast(T, p1)));
+  const auto q = __builtin_amdgcn_permlane16_swap(y, y, false, false);
+  const uint32_t q0 = q[0], q1 = q[1];
+  return op(__builtin_bit_cast(T, q0), __builtin_bit_cast(T, q1));
+}
 __device__ __forceinline__ Cand wave_best(Cand c) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const Cand x = {__shfl_xor(c.z, o, 64), (uint32_t)__shfl_xor((int)c.id, o, 64)};
-    if (better(x, c)) c = x;
-  }
-  return c;
+  const float z = wave_reduce(c.z, [](float x, float y) { return fmaxf(x, y); });
+  return {z, wave_reduce(c.z == z ? c.id : kNone, [](uint32_t x, uint32_t y) { return min(x, y); })};
+}
+
+// Place k of the list of (row, split). The rows of a block lie side by side: a workgroup's threads, one per row, read
+// and write whole lines. (With a row's splits side by side, 256 of them, every access was a page of its own.)
+__device__ __forceinline__ int64_t lp_list(const LpArgs& a, int row, int split, int k) {
+  const int blocks = (a.rows + a.block - 1) / a.block;
+  return (((int64_t)split * blocks + row / a.block) * a.top + k) * a.block + row % a.block;
 }
 
 // Joins (m2, s2, t2) into (m, s, t). An empty side is (-inf, 0, 0).
@@ -72,6 +97,29 @@ __global__ __launch_bounds__(256) void lp_logits_bf16_kernel(LpArgs a, int tiles
           *reinterpret_cast<f32x4*>(a.logits + (int64_t)t * a.ldz + v) =
               f32x4{acc[i][j][r], acc[i][j][r + 1], acc[i][j][r + 2], acc[i][j][r + 3]};
       }
+  }
+}
+
+// The same with 256 x 256 tiles on eight waves, for more than 128 rows.
+__global__ __launch_bounds__(512) void lp_logits_big_kernel(LpArgs a, int tiles_v, int tiles_t) {
+  using C = CfgBig;
+  extern __shared__ __align__(16) uint8_t smem[];
+  int tv, tt;
+  tile_of(blockIdx.x, tiles_v, tiles_t, tv, tt);
+  const int v0 = tv * 256, t0 = tt * 256;
+  Acc16 acc;
+  mfma_mainloop_pp16<C>(static_cast<const bf16_t*>(a.W) + (int64_t)v0 * a.d, a.d, a.V - v0,
+                        static_cast<const bf16_t*>(a.h) + (int64_t)(a.row0 + t0) * a.d, a.d, a.rows - t0, a.d,
+                        reinterpret_cast<bf16_t*>(smem), acc);
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int vb = v0 + (w >> 2) * 128 + 4 * (lane >> 4);
+#pragma unroll
+  for (int j = 0; j < Mma16::TN; ++j) {
+    const int t = t0 + (w & 3) * 64 + 16 * j + (lane & 15);
+    if (t >= a.rows) continue;
+#pragma unroll
+    for (int i = 0; i < Mma16::TM; ++i)
+      if (vb + 16 * i < a.V) *reinterpret_cast<f32x4*>(a.logits + (int64_t)t * a.ldz + vb + 16 * i) = acc[i][j];
   }
 }
 
@@ -131,28 +179,33 @@ __global__ __launch_bounds__(256) void lp_logits_f32_kernel(LpArgs a, int tiles_
 // The logits of a row tile of 256 tokens without memory for them: a persistent workgroup walks the vocabulary tiles split,
 // split + splits, ... of the product z^T = W h^T (gemm_core.hpp's 256 x 256 tiles on eight waves) and takes what it
 // needs from each while the next tile's first loads are on their way. A lane holds 32 logits of each of 4 tokens.
-// Statistics: every token's (m, s, t) per half of the tile's rows (wave row), kept in LDS.
-// Alternatives: a token's list of the best so far lies in its place of `lists`, the last of it as a threshold in LDS.
-// A tile's logits above the threshold are handed to the token's thread through kHand places in LDS, in as
-// many rounds as it takes; that thread sorts them into the list and raises the threshold. After the first tile
-// there are few: a tile of M replaces about top / M of them. Ids grow from tile to tile, so that a logit equal to the
-// threshold never displaces an earlier one; within a tile the ids decide. The list does not depend on
-// the order in which candidates arrive.
-constexpr int kHand = 8;
+// Statistics: every token's (m, s, t) per half of the tile's rows (wave row), in LDS.
+// Alternatives: every token's best so far lie sorted in LDS as one 64-bit key each, larger for the larger logit and
+// among equal ones for the lower id. A logit above the last of them enters at the top: an atomic maximum leaves
+// the larger key in a place and takes the smaller one on to the next. Each place passes on all keys but the
+// largest that it meets, so the list does not depend on the order in which keys arrive, and needs no barrier. After the
+// first tile there are few: a tile of M replaces about top / M of a token's list. In the first, a bisection finds a
+// bound that `top` of the wave's logits of a token reach, and the rest stay out.
 struct LpFusedLds {
   float m[2][256], s[2][256], t[2][256];
-  float zy[256];        // the label's logit; NaN until it has been met
-  int32_t y[256];       // the label; negative: none in the vocabulary
-  float thr[256];       // the list's last logit; NaN: the list is not full; +inf: no list
-  uint32_t thr_id[256]; // and its id
-  int32_t count[256];   // candidates of the round, kHand of which have a place
-  Cand hand[256][kHand];
+  float zy[256];   // the label's logit; NaN until it has been met
+  int32_t y[256];  // the label; negative: none in the vocabulary
+  uint64_t best[kLpFusedTop][256];  // 0: none
 };
 constexpr size_t kLpFusedLds = CfgBig::LDS + sizeof(LpFusedLds);
 static_assert(kLpFusedLds <= 160 * 1024, "LDS");
 
-// KB: places of a list (0: no alternatives)
-template <int KB>
+__device__ __forceinline__ uint64_t cand_key(float z, uint32_t id) {
+  const uint32_t b = __float_as_uint(z + 0.0f);  // -0 is 0
+  return (uint64_t)(b >> 31 ? ~b : b | 0x80000000u) << 32 | ~id;
+}
+__device__ __forceinline__ Cand key_cand(uint64_t key) {
+  if (key == 0) return {-INFINITY, kNone};
+  const uint32_t b = (uint32_t)(key >> 32);
+  return {__uint_as_float(b >> 31 ? b & 0x7FFFFFFFu : ~b), ~(uint32_t)key};
+}
+
+template <bool TOP>
 __global__ __launch_bounds__(512) void lp_fused_kernel(LpArgs a, int tiles_t, int tiles_v) {
   using C = CfgBig;
   extern __shared__ __align__(16) uint8_t smem[];
@@ -168,9 +221,8 @@ __global__ __launch_bounds__(512) void lp_fused_kernel(LpArgs a, int tiles_t, in
     L.zy[tid] = __uint_as_float(0x7FC00000u);
     const int y = tid < nt ? a.labels[a.row0 + t0 + tid] : -1;
     L.y[tid] = y < a.V ? y : -1;
-    L.thr[tid] = tid < nt ? __uint_as_float(0x7FC00000u) : INFINITY;
-    L.thr_id[tid] = kNone;
-    L.count[tid] = 0;
+    if constexpr (TOP)
+      for (int k = 0; k < a.top; ++k) L.best[k][tid] = 0;
   }
   const bf16_t* W = static_cast<const bf16_t*>(a.W);
   const bf16_t* h = static_cast<const bf16_t*>(a.h) + (int64_t)(a.row0 + t0) * a.d;
@@ -189,11 +241,11 @@ __global__ __launch_bounds__(512) void lp_fused_kernel(LpArgs a, int tiles_t, in
     const int lane = id & 63, w = __builtin_amdgcn_readfirstlane(id >> 6);
     const int wm = w >> 2, l16 = lane & 15, q4 = lane >> 4;
     const int vb = v0 + wm * 128 + 4 * q4;  // entry (i, r) of the lane: vb + 16 i + r
-    uint32_t pending[Mma16::TN];            // bit 4 i + r
     const bool whole = v0 + 256 <= a.V;
 #pragma unroll
     for (int j = 0; j < Mma16::TN; ++j) {
       const int tok = (w & 3) * 64 + 16 * j + l16;
+      if ((w & 3) * 64 + 16 * j >= nt) break;  // rows past the last
       if (!whole) {
 #pragma unroll
         for (int i = 0; i < Mma16::TM; ++i)
@@ -206,7 +258,8 @@ __global__ __launch_bounds__(512) void lp_fused_kernel(LpArgs a, int tiles_t, in
       for (int i = 0; i < Mma16::TM; ++i)
 #pragma unroll
         for (int r = 0; r < 4; ++r) mx = fmaxf(mx, acc[i][j][r]);
-      const float m_old = L.m[wm][tok], m = fmaxf(m_old, rows_max(mx));
+      mx = rows_max(mx);
+      const float m_old = L.m[wm][tok], m = fmaxf(m_old, mx);
       const float m0 = m == -INFINITY ? 0.0f : m;
       const float mb = m0 * kLog2e;
       float s = 0.0f, t = 0.0f;
@@ -222,16 +275,20 @@ __global__ __launch_bounds__(512) void lp_fused_kernel(LpArgs a, int tiles_t, in
       t = rows_sum(t);
       const float s_old = L.s[wm][tok], t_old = L.t[wm][tok];
       const float dm = m_old == -INFINITY ? 0.0f : m_old - m0, f = __builtin_amdgcn_exp2f(dm * kLog2e);
-      const int y = L.y[tok] - (v0 + wm * 128);
-      const bool has = y >= 0 && y < 128 && (y >> 2 & 3) == q4;
-      if (__any(has)) {
-        const int e = (y >> 4) * 4 + (y & 3);
+      // entry e of the lane's 32
+      auto entry = [&](uint32_t e) {
         float z = 0.0f;
 #pragma unroll
         for (int i = 0; i < Mma16::TM; ++i)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (e == 4 * i + r) z = acc[i][j][r];
+            if (e == 4u * i + r) z = acc[i][j][r];
+        return z;
+      };
+      const int y = L.y[tok] - (v0 + wm * 128);
+      const bool has = y >= 0 && y < 128 && (y >> 2 & 3) == q4;
+      if (__any(has)) {
+        const float z = entry((y >> 4) * 4 + (y & 3));
         if (has) L.zy[tok] = z;
       }
       // all of the wave's reads of the token's old values come before the writes
@@ -240,84 +297,42 @@ __global__ __launch_bounds__(512) void lp_fused_kernel(LpArgs a, int tiles_t, in
         L.s[wm][tok] = s_old * f + s;
         L.t[wm][tok] = (t_old + dm * s_old) * f + t;
       }
-      if constexpr (KB > 0) {
-        const float thr = L.thr[tok];
+      if constexpr (TOP) {
+        const uint64_t last = L.best[a.top - 1][tok];
+        float thr = last == 0 ? -INFINITY : key_cand(last).z;
+        bool full = last != 0;  // a logit has to be above thr, or else at it
+        if (first) {
+          float a1 = mx, a0 = mx - 32.0f;
+#pragma unroll 1
+          for (int n = 0; n < 10; ++n) {
+            const float mid = n == 0 ? a0 : 0.5f * (a0 + a1);
+            float c = 0.0f;
+#pragma unroll
+            for (int i = 0; i < Mma16::TM; ++i)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) c += acc[i][j][r] >= mid ? 1.0f : 0.0f;
+            const bool enough = rows_sum(c) >= (float)a.top;
+            thr = enough && !full ? fmaxf(thr, mid) : thr;
+            a0 = enough ? mid : a0;
+            a1 = enough ? a1 : mid;
+          }
+        }
         uint32_t p = 0;
 #pragma unroll
         for (int i = 0; i < Mma16::TM; ++i)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (!(acc[i][j][r] <= thr) && (whole || vb + 16 * i + r < a.V)) p |= 1u << (4 * i + r);
-        pending[j] = p;
-      }
-    }
-    if constexpr (KB > 0) {
-      for (;;) {
-#pragma unroll
-        for (int j = 0; j < Mma16::TN; ++j) {
-          const int tok = (w & 3) * 64 + 16 * j + l16;
-          if (pending[j]) {
-#pragma unroll
-            for (int i = 0; i < Mma16::TM; ++i)
-#pragma unroll
-              for (int r = 0; r < 4; ++r)
-                if (pending[j] >> (4 * i + r) & 1) {
-                  const int at = atomicAdd(&L.count[tok], 1);
-                  if (at < kHand) {
-                    L.hand[tok][at] = {acc[i][j][r], (uint32_t)(vb + 16 * i + r)};
-                    pending[j] &= ~(1u << (4 * i + r));
-                  }
-                }
-          }
-        }
-        __syncthreads();
-        bool more = false;
-        const int n = id < 256 ? L.count[id] : 0;
-        if (n > 0) {
-          more = n > kHand;
-          Cand list[KB];
-          float2* mine = a.lists + ((int64_t)(t0 + id) * a.splits + split) * KB;
-          const bool fresh = first && L.thr_id[id] == kNone;  // nothing has been written yet
-#pragma unroll
-          for (int k = 0; k < KB; ++k) {
-            const float2 x = fresh ? make_float2(-INFINITY, __uint_as_float(kNone)) : mine[k];
-            list[k] = {x.x, __float_as_uint(x.y)};
-          }
-          bool nan = false;
-#pragma unroll 1
-          for (int c = 0; c < min(n, kHand); ++c) {
-            Cand x = L.hand[id][c];
-            nan |= x.z != x.z;
-#pragma unroll
-            for (int k = 0; k < KB; ++k) {
-              const bool up = better(x, list[k]);
-              const Cand y = up ? list[k] : x;
-              list[k] = up ? x : list[k];
-              x = y;
+            if ((acc[i][j][r] > thr || (!full && acc[i][j][r] == thr)) && (whole || vb + 16 * i + r < a.V)) p |= 1u << (4 * i + r);
+        if (tok >= nt) p = 0;
+        while (__any(p != 0)) {
+          const uint32_t e = p ? __builtin_ctz(p) : 0;
+          uint64_t key = cand_key(entry(e), (uint32_t)(vb + (e >> 2) * 16 + (e & 3)));
+          if (p != 0 && key > L.best[a.top - 1][tok])
+            for (int k = 0; k < a.top && key != 0; ++k) {
+              const uint64_t was = atomicMax(reinterpret_cast<unsigned long long*>(&L.best[k][tok]), (unsigned long long)key);
+              key = was < key ? was : key;
             }
-          }
-          Cand last = list[0];
-#pragma unroll
-          for (int k = 0; k < KB; ++k) {
-            mine[k] = make_float2(list[k].z, __uint_as_float(list[k].id));
-            if (k == a.top - 1) last = list[k];
-          }
-          // an id marks the list as written even while it is not full
-          L.thr[id] = nan ? INFINITY : last.id == kNone ? __uint_as_float(0x7FC00000u) : last.z;
-          L.thr_id[id] = last.id == kNone ? kNone - 1 : last.id;
-          L.count[id] = 0;
-        }
-        if (!__syncthreads_or(more)) break;
-#pragma unroll
-        for (int j = 0; j < Mma16::TN; ++j) {
-          const int tok = (w & 3) * 64 + 16 * j + l16;
-          const float thr = L.thr[tok];
-          const uint32_t ti = L.thr_id[tok];
-#pragma unroll
-          for (int i = 0; i < Mma16::TM; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (acc[i][j][r] < thr || (acc[i][j][r] == thr && (uint32_t)(vb + 16 * i + r) > ti)) pending[j] &= ~(1u << (4 * i + r));
+          p &= p - 1;
         }
       }
     }
@@ -326,11 +341,12 @@ __global__ __launch_bounds__(512) void lp_fused_kernel(LpArgs a, int tiles_t, in
   if (tid < nt) {
     float m = L.m[0][tid], s = L.s[0][tid], t = L.t[0][tid];
     stats_join(m, s, t, L.m[1][tid], L.s[1][tid], L.t[1][tid]);
-    const int64_t at = (int64_t)(t0 + tid) * a.splits + split;
-    a.stats[at] = make_float4(m, s, t, L.zy[tid]);
-    if constexpr (KB > 0)
-      if (L.thr_id[tid] == kNone)  // not one candidate
-        for (int k = 0; k < KB; ++k) a.lists[at * KB + k] = make_float2(-INFINITY, __uint_as_float(kNone));
+    a.stats[(int64_t)split * a.rows + t0 + tid] = make_float4(m, s, t, L.zy[tid]);
+    if constexpr (TOP)
+      for (int k = 0; k < a.top; ++k) {
+        const Cand c = key_cand(L.best[k][tid]);
+        a.lists[lp_list(a, t0 + tid, split, k)] = make_float2(c.z, __uint_as_float(c.id));
+      }
   }
 }
 
@@ -369,11 +385,10 @@ __global__ __launch_bounds__(256) void lp_rows_kernel(LpArgs a) {
   __shared__ Cand best[2][4];
   if (lane == 0) st[w] = make_float4(m, s, t, 0.0f);
   __syncthreads();
-  const int64_t at = (int64_t)row * a.splits + split;
   if (tid == 0) {
     for (int i = 1; i < 4; ++i) stats_join(m, s, t, st[i].x, st[i].y, st[i].z);
     const int y = a.labels[a.row0 + row];
-    a.stats[at] = make_float4(m, s, t, y >= v0 && y < min(a.V, v0 + kLpRowChunk) ? z[y] : __uint_as_float(0x7FC00000u));
+    a.stats[(int64_t)split * a.rows + row] = make_float4(m, s, t, y >= v0 && y < min(a.V, v0 + kLpRowChunk) ? z[y] : __uint_as_float(0x7FC00000u));
   }
   uint32_t taken = 0;
   auto mine = [&]() {
@@ -395,7 +410,7 @@ __global__ __launch_bounds__(256) void lp_rows_kernel(LpArgs a) {
 #pragma unroll
     for (int i = 1; i < 4; ++i)
       if (better(best[n & 1][i], b)) b = best[n & 1][i];
-    if (tid == 0) a.lists[at * a.places + n] = make_float2(b.z, __uint_as_float(b.id));
+    if (tid == 0) a.lists[lp_list(a, row, split, n)] = make_float2(b.z, __uint_as_float(b.id));
     if (b.id != kNone && b.id == c.id) {
       const int rel = (int)b.id - v0;
       taken |= 1u << (rel / 1024 * 4 + (rel & 3));
@@ -404,14 +419,21 @@ __global__ __launch_bounds__(256) void lp_rows_kernel(LpArgs a) {
   }
 }
 
-// Joins a row's splits and writes its results. One wave per row.
+// Joins a row's splits and writes its results: T threads per row (a wave, or the workgroup where there are
+// more splits than lanes). The splits' lists are sorted, so a thread holds the head of its list, with the one
+// behind it on its way, and the best head of all is drawn `top` times. (One wave that looked through all lists for
+// every draw took 0.9 ms for 20 of 256 x 20 candidates.)
+template <int T>
 __global__ __launch_bounds__(256) void lp_join_kernel(LpArgs a) {
-  const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= a.rows) return;
-  const int64_t at = (int64_t)row * a.splits, out = a.row0 + row;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, id = threadIdx.x % T;
+  const int row = blockIdx.x * (256 / T) + threadIdx.x / T;
+  if (T == 64 && row >= a.rows) return;
+  __shared__ float4 parts[4];
+  __shared__ Cand heads[2][4];
+  const int64_t out = a.row0 + row;
   float m = -INFINITY, s = 0.0f, t = 0.0f, zy = __uint_as_float(0x7FC00000u);
-  for (int i = lane; i < a.splits; i += 64) {
-    const float4 x = a.stats[at + i];
+  for (int i = id; i < a.splits; i += T) {
+    const float4 x = a.stats[(int64_t)i * a.rows + row];
     stats_join(m, s, t, x.x, x.y, x.z);
     if (x.w == x.w) zy = x.w;
   }
@@ -421,27 +443,58 @@ __global__ __launch_bounds__(256) void lp_join_kernel(LpArgs a) {
     const float other = __shfl_xor(zy, o, 64);
     if (other == other) zy = other;
   }
+  if constexpr (T > 64) {
+    if (lane == 0) parts[w] = make_float4(m, s, t, zy);
+    __syncthreads();
+    m = parts[0].x, s = parts[0].y, t = parts[0].z, zy = parts[0].w;
+    for (int i = 1; i < T / 64; ++i) {
+      stats_join(m, s, t, parts[i].x, parts[i].y, parts[i].z);
+      if (parts[i].w == parts[i].w) zy = parts[i].w;
+    }
+  }
   const float ls = logf(s), lse = m + ls;
-  if (lane == 0) {
+  if (id == 0) {
     a.logp[out] = zy - lse;
     if (a.entropy) a.entropy[out] = ls - t / s;
   }
-  // the best of the lists, one after the other; a row that has no finite lse has none
-  const int n = a.splits * a.top;
-  Cand last = {INFINITY, 0};
-  bool first = true;
+  auto entry = [&](int list, int k) -> Cand {
+    if (list >= a.splits || k >= a.top) return {-INFINITY, kNone};
+    const float2 x = a.lists[lp_list(a, row, list, k)];
+    return {x.x, __float_as_uint(x.y)};
+  };
+  // The thread's best, which `last` has drawn from: the next of its list, or, with several lists, the best behind `last`.
+  const bool one = a.splits <= T;
+  Cand head = entry(id, 0), next = entry(id, 1);
+  int k_next = 2;
+  auto search = [&](bool all, Cand last) {
+    head = {-INFINITY, kNone};
+    for (int list = id; list < a.splits; list += T)
+      for (int k = 0; k < a.top; ++k) {
+        const Cand c = entry(list, k);
+        if ((all || better(last, c)) && better(c, head)) head = c;
+      }
+  };
+  if (!one) search(true, head);
   for (int k = 0; k < a.top; ++k) {
-    Cand c = {-INFINITY, kNone};
-    for (int i = lane; i < n; i += 64) {
-      const float2 x = a.lists[(at + i / a.top) * a.places + i % a.top];
-      const Cand y = {x.x, __float_as_uint(x.y)};
-      if (y.id != kNone && (first || better(last, y)) && better(y, c)) c = y;
+    Cand c = wave_best(head);
+    if constexpr (T > 64) {
+      if (lane == 0) heads[k & 1][w] = c;
+      __syncthreads();
+      c = heads[k & 1][0];
+#pragma unroll
+      for (int i = 1; i < T / 64; ++i)
+        if (better(heads[k & 1][i], c)) c = heads[k & 1][i];
     }
-    c = wave_best(c);
-    last = c;
-    first = false;
-    if (lane == 0) {
-      const bool ok = __builtin_isfinite(lse) && c.id != kNone;
+    if (c.id == head.id && c.id != kNone) {
+      if (one) {
+        head = next;
+        next = entry(id, k_next++);
+      } else {
+        search(false, c);
+      }
+    }
+    if (id == 0) {
+      const bool ok = __builtin_isfinite(lse) && c.id != kNone;  // a row that has no finite lse has no alternatives
       a.top_ids[out * a.top + k] = ok ? (int32_t)c.id : -1;
       a.top_logp[out * a.top + k] = ok ? c.z - lse : __uint_as_float(0x7FC00000u);
     }
@@ -450,7 +503,12 @@ __global__ __launch_bounds__(256) void lp_join_kernel(LpArgs a) {
 
 hipError_t launch_lp_logits(int dtype, const LpArgs& a, hipStream_t s) {
   KernelTimer t(K_LP_LOGITS, s);
-  if (dtype == 1) {
+  if (dtype == 1 && a.rows > 128) {
+    static LdsLimit limit;
+    if (hipError_t e = limit.raise((const void*)lp_logits_big_kernel, CfgBig::LDS)) return e;
+    const int tv = (a.V + 255) / 256, tt = (a.rows + 255) / 256;
+    hipLaunchKernelGGL(lp_logits_big_kernel, dim3(tv * tt), dim3(512), CfgBig::LDS, s, a, tv, tt);
+  } else if (dtype == 1) {
     static LdsLimit limit;
     if (hipError_t e = limit.raise((const void*)lp_logits_bf16_kernel, CfgSmall::LDS)) return e;
     const int tv = (a.V + CfgSmall::BM - 1) / CfgSmall::BM, tt = (a.rows + CfgSmall::BN - 1) / CfgSmall::BN;
@@ -462,19 +520,17 @@ hipError_t launch_lp_logits(int dtype, const LpArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <int KB>
+template <bool TOP>
 static hipError_t launch_fused(const LpArgs& a, hipStream_t s) {
   static LdsLimit limit;
-  if (hipError_t e = limit.raise((const void*)lp_fused_kernel<KB>, kLpFusedLds)) return e;
+  if (hipError_t e = limit.raise((const void*)lp_fused_kernel<TOP>, kLpFusedLds)) return e;
   const int tiles_t = (a.rows + 255) / 256, tiles_v = (a.V + 255) / 256;
   KernelTimer t(K_LP_FUSED, s);
-  hipLaunchKernelGGL(lp_fused_kernel<KB>, dim3(tiles_t * a.splits), dim3(512), kLpFusedLds, s, a, tiles_t, tiles_v);
+  hipLaunchKernelGGL(lp_fused_kernel<TOP>, dim3(tiles_t * a.splits), dim3(512), kLpFusedLds, s, a, tiles_t, tiles_v);
   return hipGetLastError();
 }
 
-hipError_t launch_lp_fused(const LpArgs& a, hipStream_t s) {
-  return a.top == 0 ? launch_fused<0>(a, s) : a.places == 8 ? launch_fused<8>(a, s) : a.places == 16 ? launch_fused<16>(a, s) : launch_fused<32>(a, s);
-}
+hipError_t launch_lp_fused(const LpArgs& a, hipStream_t s) { return a.top ? launch_fused<true>(a, s) : launch_fused<false>(a, s); }
 
 hipError_t launch_lp_rows(const LpArgs& a, hipStream_t s) {
   KernelTimer t(K_LP_ROWS, s);
@@ -484,7 +540,10 @@ hipError_t launch_lp_rows(const LpArgs& a, hipStream_t s) {
 
 hipError_t launch_lp_join(const LpArgs& a, hipStream_t s) {
   KernelTimer t(K_LP_JOIN, s);
-  hipLaunchKernelGGL(lp_join_kernel, dim3((a.rows + 3) / 4), dim3(256), 0, s, a);
+  if (a.splits <= 64)
+    hipLaunchKernelGGL(lp_join_kernel<64>, dim3((a.rows + 3) / 4), dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL(lp_join_kernel<256>, dim3(a.rows), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
