@@ -232,7 +232,7 @@ constexpr int64_t kLpFusedRows = 65536;   // rows of a launch without staging, w
 struct LpPlan {
   bool fused = false;          // no staged logits
   int64_t ldz = 0, rows = 0;   // staged logits: row length; rows at a time
-  int32_t splits = 0, block = 0;
+  int32_t splits = 0, block = 0, chunk = 0;
   size_t off_stats = 0, off_lists = 0, total = 0;
 };
 
@@ -250,6 +250,9 @@ attt_status lp_check(int64_t N, int64_t d, int64_t V, int32_t dtype, int32_t top
 
 LpPlan lp_plan(int64_t N, int64_t V, int32_t dtype, int32_t top) {
   LpPlan P;
+  // Without staging a workgroup's first tile and its list cost about 50 us with alternatives, staging the writing and
+  // reading of N x V logits. Staged / not, 8 alternatives, in us: 128256 entries, 128 rows 266 / 305, 256 rows 325 / 319, 1024
+  // rows 1144 / 891; 32000 entries, 256 rows 83 / 92, 512 rows 107 / 104; 5000 entries, 512 rows 58 / 72.
   P.fused = dtype == ATTT_BF16 && top <= kLpFusedTop && N > 128 && (top == 0 || N * V >= 10000000);
   if (P.fused) {
     P.rows = std::min(N, kLpFusedRows);
@@ -267,7 +270,11 @@ LpPlan lp_plan(int64_t N, int64_t V, int32_t dtype, int32_t top) {
     // rows of about 256 MiB of logits at a time
     const int64_t fit = ((int64_t)256 << 20) / (P.ldz * 4);
     P.rows = std::min<int64_t>(std::max<int64_t>(N, 1), fit >= 128 ? fit / 128 * 128 : std::max<int64_t>(1, fit));
-    P.splits = (int32_t)ceil_div(V, kLpRowChunk);
+    // Every workgroup draws its list one by one: few long chunks where the rows fill the chip anyway and V fills the
+    // chunks. 20 alternatives with short and long chunks, in us: 128256 entries, 16 rows 218 and 224, 128 rows 308 and
+    // 294, 1024 rows 1470 and 1301; 5000 entries, 2048 rows 129 and 151.
+    P.chunk = kLpRowChunk[V >= kLpRowChunk[1] && P.rows * ceil_div(V, kLpRowChunk[0]) > 1024];
+    P.splits = (int32_t)ceil_div(V, P.chunk);
     P.block = (int32_t)P.rows;
   }
   P.off_stats = align256((size_t)P.rows * P.ldz * 4);
@@ -319,6 +326,7 @@ extern "C" attt_status attt_token_logprobs(const void* hidden, const void* lm_he
   a.top = top;
   a.splits = P.splits;
   a.block = P.block;
+  a.chunk = P.chunk;
   hipStream_t s = static_cast<hipStream_t>(stream);
   for (int64_t r0 = 0; r0 < N; r0 += P.rows) {
     a.row0 = (int32_t)r0;

@@ -233,7 +233,7 @@ hipError_t launch_kv4_attention(int row_tiles, const Kv4Args& a, const Kv4Batch&
 // ---- log-probabilities of given tokens -------------------------------------------------------------
 constexpr int kLpMaxTop = 32;       // most alternatives
 constexpr int kLpFusedTop = 10;      // most alternatives that have a place in LDS beside the product's tiles
-constexpr int kLpRowChunk = 4096;   // logits a workgroup of the row kernel takes
+constexpr int kLpRowChunk[2] = {4096, 16384};  // logits a workgroup of the row kernel takes
 struct LpArgs {
   const void* h;         // [N][d]
   const void* W;         // [V][d]
@@ -248,7 +248,7 @@ struct LpArgs {
   int64_t ldz;
   int32_t N, d, V, top;
   int32_t row0, rows;    // the rows of the launch
-  int32_t splits, block;
+  int32_t splits, block, chunk;
 };
 hipError_t launch_lp_logits(int dtype, const LpArgs& a, hipStream_t s);
 // bf16, top <= kLpFusedTop: statistics and lists of `splits` parts of the vocabulary, without staged logits

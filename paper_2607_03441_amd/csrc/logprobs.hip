@@ -350,15 +350,17 @@ __global__ __launch_bounds__(512) void lp_fused_kernel(LpArgs a, int tiles_t, in
   }
 }
 
-// Statistics and the best `top` of kLpRowChunk logits of one staged row: 16 a thread, in registers. The best
-// are drawn one after the other: the best of each thread's, of each wave's, of the workgroup's.
+// Statistics and the best `top` of 256 E logits of one staged row, E a thread, in registers. The best are drawn one
+// after the other: the best of each thread's, of each wave's, of the workgroup's; a thread keeps the best of
+// every 16, so that a draw costs its owner one scan of 16.
+template <int E>
 __global__ __launch_bounds__(256) void lp_rows_kernel(LpArgs a) {
-  constexpr int E = kLpRowChunk / 256;
+  constexpr int G = E / 16;
   const int row = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const float* z = a.logits + (int64_t)row * a.ldz;
-  const int v0 = split * kLpRowChunk;
-  float x[E];
+  const int v0 = split * (256 * E);
+  float x[E];  // entry i: v0 + (i / 4 * 256 + tid) * 4 + i % 4; past the row -inf
   float m = -INFINITY;
 #pragma unroll
   for (int i = 0; i < E; i += 4) {
@@ -388,20 +390,31 @@ __global__ __launch_bounds__(256) void lp_rows_kernel(LpArgs a) {
   if (tid == 0) {
     for (int i = 1; i < 4; ++i) stats_join(m, s, t, st[i].x, st[i].y, st[i].z);
     const int y = a.labels[a.row0 + row];
-    a.stats[(int64_t)split * a.rows + row] = make_float4(m, s, t, y >= v0 && y < min(a.V, v0 + kLpRowChunk) ? z[y] : __uint_as_float(0x7FC00000u));
+    a.stats[(int64_t)split * a.rows + row] =
+        make_float4(m, s, t, y >= v0 && y < min(a.V, v0 + 256 * E) ? z[y] : __uint_as_float(0x7FC00000u));
   }
-  uint32_t taken = 0;
-  auto mine = [&]() {
+  if (a.top == 0) return;
+  // what is drawn, or past the row, becomes a NaN, which is better than nothing else
+  auto entry = [&](int i) { return (uint32_t)(v0 + (i / 4 * 256 + tid) * 4 + (i & 3)); };
+  auto scan = [&](int g, uint32_t drawn) {
     Cand c = {-INFINITY, kNone};
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-      const int v = v0 + (i / 4 * 256 + tid) * 4 + (i & 3);
-      const Cand k = {x[i], (uint32_t)v};
-      if (v < a.V && !(taken >> i & 1) && better(k, c)) c = k;
+    for (int i = 16 * g; i < 16 * g + 16; ++i) {
+      if (entry(i) == drawn) x[i] = __uint_as_float(0x7FC00000u);
+      const Cand k = {x[i], entry(i)};
+      if (better(k, c)) c = k;
     }
     return c;
   };
-  Cand c = a.top > 0 ? mine() : Cand{};
+  Cand group[G], c = {-INFINITY, kNone};
+#pragma unroll
+  for (int i = 0; i < E; ++i)
+    if (entry(i) >= (uint32_t)a.V) x[i] = __uint_as_float(0x7FC00000u);
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    group[g] = scan(g, kNone);
+    if (better(group[g], c)) c = group[g];
+  }
   for (int n = 0; n < a.top; ++n) {
     const Cand wb = wave_best(c);
     if (lane == 0) best[n & 1][w] = wb;
@@ -412,9 +425,12 @@ __global__ __launch_bounds__(256) void lp_rows_kernel(LpArgs a) {
       if (better(best[n & 1][i], b)) b = best[n & 1][i];
     if (tid == 0) a.lists[lp_list(a, row, split, n)] = make_float2(b.z, __uint_as_float(b.id));
     if (b.id != kNone && b.id == c.id) {
-      const int rel = (int)b.id - v0;
-      taken |= 1u << (rel / 1024 * 4 + (rel & 3));
-      c = mine();
+      c = {-INFINITY, kNone};
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        if (group[g].id == b.id) group[g] = scan(g, b.id);
+        if (better(group[g], c)) c = group[g];
+      }
     }
   }
 }
@@ -534,7 +550,10 @@ hipError_t launch_lp_fused(const LpArgs& a, hipStream_t s) { return a.top ? laun
 
 hipError_t launch_lp_rows(const LpArgs& a, hipStream_t s) {
   KernelTimer t(K_LP_ROWS, s);
-  hipLaunchKernelGGL(lp_rows_kernel, dim3((unsigned)a.rows * a.splits), dim3(256), 0, s, a);
+  if (a.chunk == 16 * 256)
+    hipLaunchKernelGGL(lp_rows_kernel<16>, dim3((unsigned)a.rows * a.splits), dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL(lp_rows_kernel<64>, dim3((unsigned)a.rows * a.splits), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
