@@ -65,14 +65,12 @@ attt_status kv4_table(const int32_t* table, int64_t width, const int32_t* length
   return ATTT_OK;
 }
 
-// The attention's launch: tiles of 16 query rows per workgroup, and how many pages a split of a sequence has.
-// A tile costs a workgroup 64 registers per lane and its own products, while every tile reads the page again where
-// the rows are cut into more workgroups.
+// The attention's launch: the query rows of a head's group that a workgroup takes, and how many pages a split has.
 struct Kv4Plan {
-  int32_t row_tiles = 1, chunk = 1, splits = 1;
+  int32_t block_rows = 16, chunk = 1, splits = 1;
   int64_t units = 0;
   size_t bytes() const {
-    return splits > 1 ? (size_t)units * splits * 16 * row_tiles * (128 * sizeof(float) + sizeof(float2)) : 0;
+    return splits > 1 ? (size_t)units * splits * block_rows * (128 * sizeof(float) + sizeof(float2)) : 0;
   }
 };
 
@@ -81,12 +79,13 @@ Kv4Plan kv4_plan(const Rows& rows, int32_t E, int32_t heads, int32_t kv_heads, i
   const int64_t g = heads / kv_heads;
   int64_t most = 0;
   for (int32_t e = 0; e < E; ++e) most = std::max(most, rows.count(e) * g);
-  P.row_tiles = most <= 16 ? 1 : most <= 32 ? 2 : 4;
-  for (int32_t e = 0; e < E; ++e) P.units += ceil_div(rows.count(e) * g, 16 * P.row_tiles) * kv_heads;
+  P.block_rows = most <= 16 ? 16 : most <= 64 ? 64 : 128;
+  for (int32_t e = 0; e < E; ++e) P.units += ceil_div(rows.count(e) * g, P.block_rows) * kv_heads;
   const int64_t pages = std::max<int64_t>(1, ceil_div(max_length, kKv4Page));
-  // four waves take a split's pages in turn; about four workgroups per CU
-  const int64_t chunk = std::max<int64_t>(4, round_up(ceil_div(pages * P.units, 1024), 4));
-  P.chunk = (int32_t)std::min(chunk, round_up(pages, 4));
+  // Workgroups of 16 rows take four pages at a time, one a wave, the others one.
+  const int64_t step = P.block_rows == 16 ? 4 : 1, wanted = P.block_rows == 16 ? 1024 : 512;
+  const int64_t chunk = std::max(step, round_up(ceil_div(pages * P.units, wanted), step));
+  P.chunk = (int32_t)std::min(chunk, round_up(pages, step));
   P.splits = (int32_t)ceil_div(pages, P.chunk);
   return P;
 }
@@ -210,14 +209,15 @@ extern "C" attt_status attt_kv4_attention(const void* q, const void* cache, int6
   a.kv_heads = kv_heads;
   a.chunk = P.chunk;
   a.splits = P.splits;
+  a.block_rows = P.block_rows;
   a.scale = scale;
-  const int64_t rows_part = P.units * P.splits * 16 * P.row_tiles;
+  const int64_t rows_part = P.units * P.splits * P.block_rows;
   a.part = static_cast<float*>(workspace);
   a.part_ml = P.splits > 1 ? reinterpret_cast<float2*>(a.part + rows_part * 128) : nullptr;
   int64_t blk0 = 0;
   for (int32_t e0 = 0; e0 < num_sequences; e0 += kEpBatch) {
-    const Kv4Batch b = kv4_batch(rows, e0, num_sequences, heads / kv_heads, 16 * P.row_tiles, blk0);
-    HIP_TRY(launch_kv4_attention(P.row_tiles, a, b, static_cast<hipStream_t>(stream)), "kv4_attention");
+    const Kv4Batch b = kv4_batch(rows, e0, num_sequences, heads / kv_heads, P.block_rows, blk0);
+    HIP_TRY(launch_kv4_attention(a, b, static_cast<hipStream_t>(stream)), "kv4_attention");
   }
   return ATTT_OK;
 }

@@ -212,6 +212,7 @@ struct Kv4Args {
   int64_t pages, width, max_length, N;
   int32_t heads, kv_heads;
   int32_t chunk, splits;   // pages per split, splits of the longest sequence
+  int32_t block_rows;      // query rows of a head's group per workgroup: 16, 64 or 128
   float scale;
 };
 struct Kv4Seq {
@@ -219,7 +220,7 @@ struct Kv4Seq {
   int32_t n;          // rows
   int32_t seq;        // index in table and lengths
   int32_t wg_begin;   // first workgroup (set at launch)
-  int32_t blk0;       // its first block of 16 row_tiles rows, over all sequences of the call
+  int32_t blk0;       // its first block of block_rows rows, over all sequences of the call
 };
 struct Kv4Batch {
   int32_t count;
@@ -227,8 +228,7 @@ struct Kv4Batch {
   Kv4Seq s[kEpBatch];
 };
 hipError_t launch_kv4_append(const Kv4Args& a, Kv4Batch b, hipStream_t s);
-// row_tiles (1, 2 or 4): tiles of 16 query rows of a key/value head's group per workgroup
-hipError_t launch_kv4_attention(int row_tiles, const Kv4Args& a, const Kv4Batch& b, hipStream_t s);
+hipError_t launch_kv4_attention(const Kv4Args& a, const Kv4Batch& b, hipStream_t s);
 
 // ---- log-probabilities of given tokens -------------------------------------------------------------
 constexpr int kLpMaxTop = 32;       // most alternatives

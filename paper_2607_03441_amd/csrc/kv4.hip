@@ -24,6 +24,7 @@ constexpr int DH = 128;
 constexpr int kPage = kKv4Page, kRec = kKv4Record;
 constexpr int kOffV = kPage * DH / 2, kOffKs = 2 * kOffV, kOffVs = kOffKs + kPage * 4;
 static_assert(kOffVs + kPage * 2 == kRec, "the record's parts");
+constexpr size_t kChunkBuf = kOffKs + 1024;  // a page in LDS
 constexpr float kLog2e = 1.4426950408889634f;
 
 // Where token t of a page stands in a value row.
@@ -162,60 +163,148 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Args a, Kv4Batch b) 
   }
 }
 
-// Attention of the new tokens of one (sequence, key/value head) over pages [split chunk, ..) of the sequence.
-// A wave takes whole pages in turn with the other three. The query rows of the head's group (token i,
-// query head j: row i g + j) are the columns of S^T = K Q^T, RT tiles of 16, so each lane holds scores of its own rows
-// only; per page the online softmax is a reduction over the lane's registers and its three partner
-// lanes. Weight times value scale, rounded to bf16 once, is the B operand of O^T = V^T P^T. A page's
-// keys are asked for while the one before is multiplied with its values, and its values while its keys
-// are. At the end the waves' sums are joined in a fixed order through LDS.
-template <int RT>
-__global__ __launch_bounds__(256) void kv4_attention_kernel(Kv4Args a, Kv4Batch b) {
-  constexpr int R = 16 * RT;
-  const Kv4Seq S = b.s[find_seq(b, blockIdx.x)];
-  const int local = (int)blockIdx.x - S.wg_begin;
-  const int kh = local % a.kv_heads, sb = local / a.kv_heads;
-  const int split = sb % a.splits, rb = sb / a.splits;
-  const int g = a.heads / a.kv_heads;
+namespace {
+// eight e2m1 codes times a scale as bf16 (exact)
+__device__ __forceinline__ bf16x8 widen(uint32_t x, float scale) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const bf16x2 y[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 0), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 1),
+                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 2), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 3)};
+  return bf16x8{y[0][0], y[0][1], y[1][0], y[1][1], y[2][0], y[2][1], y[3][0], y[3][1]};
+}
+
+// What a workgroup of the attention works on: rows rb R .. of a head's group (row i g + j: token i, query head j),
+// pages [p0, p1) of the sequence.
+struct Kv4Work {
+  Kv4Seq S;
+  int kh, split, rb, g, p0, p1;
+  int64_t first;  // position of the sequence's first new row
+  bool bad;       // a length beyond the bound: the rows are NaN
+  // whether there is nothing to write either
+  __device__ __forceinline__ bool locate(const Kv4Args& a, const Kv4Batch& b) {
+    S = b.s[find_seq(b, blockIdx.x)];
+    const int local = (int)blockIdx.x - S.wg_begin;
+    kh = local % a.kv_heads;
+    const int sb = local / a.kv_heads;
+    split = sb % a.splits;
+    rb = sb / a.splits;
+    g = a.heads / a.kv_heads;
+    int64_t len = a.lengths[S.seq];
+    bad = len > a.max_length;
+    if (len < 0 || bad) len = 0;
+    p0 = split * a.chunk;
+    p1 = min((int)((len + kPage - 1) / kPage), p0 + a.chunk);
+    first = len - S.n;
+    return split > 0 && p0 >= p1;  // not among those that are joined
+  }
+};
+
+// One row tile's query rows as B operands, in the order in which a lane holds its keys' codes; the last position that
+// the lane's row sees (-1: none). Rows past the sequence's are zero.
+__device__ __forceinline__ int load_rows(bf16x8 (&qf)[4], const Kv4Args& a, const Kv4Work& k, int row, int q4) {
+  const int i = row / k.g, j = row % k.g;
+  const bool on = row < k.S.n * k.g;
+  const bf16_t* src = a.q + ((k.S.row0 + (on ? i : 0)) * a.heads + k.kh * k.g + (on ? j : 0)) * DH + 32 * q4;
+#pragma unroll
+  for (int s = 0; s < 4; ++s) {
+    const u32x4 x = *reinterpret_cast<const u32x4*>(src + 8 * s);
+    qf[s] = __builtin_bit_cast(bf16x8, on ? x : u32x4{0, 0, 0, 0});
+  }
+  return on ? (int)max((int64_t)-1, k.first + i) : -1;
+}
+
+// The online softmax of PT tiles of 16 tokens, the lane's being t0 + 16 i + r, for one row tile: scores in, weights
+// times the value scales (pairs in `scale`, bf16 bits, in the order of the value rows) out, rounded to bf16 once.
+// An older maximum is replaced only where it is passed by more than 2^8.
+template <int PT, bool MASKED>
+__device__ __forceinline__ void weigh(f32x4 (&st)[PT], bf16x8 (&pw)[PT / 2], const u32x4* scale, float sl, int t0, int lim, float& m,
+                                      float& l, f32x4 (&o)[8]) {
+  float mx = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < PT; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      if constexpr (MASKED) st[i][r] = t0 + 16 * i + r <= lim ? st[i][r] : -INFINITY;
+      mx = fmaxf(mx, st[i][r]);
+    }
+  mx = rows_max(mx) * sl;
+  if (__any(mx > m + 8.0f)) {
+    const float mn = mx > m + 8.0f ? mx : m;  // per row: no other row of the tile changes it
+    const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+    m = mn;
+    l *= alpha;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] *= alpha;
+  }
+  const float ms = m == -INFINITY ? 0.0f : m;
+  float sum = 0.0f;
+  u32x4 pk[PT / 2];
+#pragma unroll
+  for (int i = 0; i < PT; ++i) {
+    float x[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const float e = __builtin_amdgcn_exp2f(fmaf(st[i][r], sl, -ms));
+      sum += e;
+      const uint32_t pair = scale[i >> 1][(i & 1) * 2 + (r >> 1)];
+      x[r] = e * __uint_as_float(r & 1 ? pair & 0xFFFF0000u : pair << 16);
+      // places that no token was written to hold any bits
+      if constexpr (MASKED) x[r] = t0 + 16 * i + r <= lim ? x[r] : 0.0f;
+    }
+    pk[i >> 1][(i & 1) * 2] = pack_bf16x2(x[0], x[1]);
+    pk[i >> 1][(i & 1) * 2 + 1] = pack_bf16x2(x[2], x[3]);
+  }
+  l += sum;
+#pragma unroll
+  for (int u = 0; u < PT / 2; ++u) pw[u] = __builtin_bit_cast(bf16x8, pk[u]);
+}
+
+// Writes a row tile's result: o and lse, or with several splits O's sums, the maximum and the sum of weights.
+__device__ __forceinline__ void write_rows(const Kv4Args& a, const Kv4Work& k, int in_block, float m, float l, const f32x4 (&o)[8], int q4) {
+  const int row = k.rb * a.block_rows + in_block, i = row / k.g, j0 = row % k.g;
+  if (row >= k.S.n * k.g) return;
+  if (a.splits > 1) {
+    const int64_t at = (((int64_t)(k.S.blk0 + k.rb) * a.kv_heads + k.kh) * a.splits + k.split) * a.block_rows + in_block;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) *reinterpret_cast<f32x4*>(a.part + at * DH + 16 * j + 4 * q4) = o[j];
+    if (q4 == 0) a.part_ml[at] = make_float2(m, l);
+    return;
+  }
+  const int h = k.kh * k.g + j0;
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;  // a row that sees nothing: 0, lse -inf
+  if (q4 == 0) a.lse[(int64_t)h * a.N + k.S.row0 + i] = l == 0.0f ? -INFINITY : m / kLog2e + logf(l);
+  bf16_t* dst = a.o + ((k.S.row0 + i) * a.heads + h) * DH + 4 * q4;
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    *reinterpret_cast<uint2*>(dst + 16 * j) = make_uint2(pack_bf16x2(o[j][0] * inv, o[j][1] * inv), pack_bf16x2(o[j][2] * inv, o[j][3] * inv));
+}
+}  // namespace
+
+// Attention of at most 16 query rows per workgroup (decoding steps): the four waves take whole pages in turn. The
+// rows are the columns of S^T = K Q^T, so each lane holds 32 scores of its own row per page; the softmax is a reduction over
+// the lane's registers and its three partner lanes. Weight times value scale is the B operand of O^T = V^T P^T. A
+// page's keys are asked for while the one before is multiplied with its values, and its values while
+// its keys are. At the end the waves' sums are joined in a fixed order through LDS.
+__global__ __launch_bounds__(256, 2) void kv4_decode_kernel(Kv4Args a, Kv4Batch b) {
+  Kv4Work k;
+  if (k.locate(a, b)) return;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, q4 = lane >> 4;
-  int64_t len = a.lengths[S.seq];
-  bool bad = len > a.max_length;
-  if (len < 0 || bad) len = 0;
-  const int used = (int)((len + kPage - 1) / kPage);
-  const int p0 = split * a.chunk, p1 = min(used, p0 + a.chunk);
-  if (split > 0 && p0 >= p1) return;  // not among those that are joined
-  const int64_t first = len - S.n;  // position of the first new row
-  bf16x8 qf[RT][4];
-  int lim[RT];  // the last position that the lane's row sees; -1: none
-#pragma unroll
-  for (int c = 0; c < RT; ++c) {
-    const int row = rb * R + 16 * c + l16, i = row / g, j = row % g;
-    const bool on = row < S.n * g;
-    lim[c] = on ? (int)max((int64_t)-1, first + i) : -1;
-    const bf16_t* src = a.q + ((S.row0 + (on ? i : 0)) * a.heads + kh * g + (on ? j : 0)) * DH + 32 * q4;
-#pragma unroll
-    for (int s = 0; s < 4; ++s)
-      qf[c][s] = on ? __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(src + 8 * s)) : bf16x8{};
-  }
-  // every row of the block sees the positions up to here
-  const int64_t all_see = first + (rb * R) / g;
+  bf16x8 qf[4];
+  const int lim = load_rows(qf, a, k, k.rb * 16 + l16, q4);
+  const int64_t all_see = k.first + (k.rb * 16) / k.g;  // every row of the block sees the positions up to here
   const float sl = a.scale * kLog2e;
-  float m[RT], l[RT];
-  f32x4 o[RT][8];
+  float m = -INFINITY, l = 0.0f;
+  f32x4 o[8];
 #pragma unroll
-  for (int c = 0; c < RT; ++c) {
-    m[c] = -INFINITY, l[c] = 0.0f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) o[c][j] = f32x4{0, 0, 0, 0};
-  }
+  for (int j = 0; j < 8; ++j) o[j] = f32x4{0, 0, 0, 0};
   u32x4 kr[8], vr[8], vs[4];
   uint2 ks;
-  const int32_t* table = a.table + (int64_t)S.seq * a.width;
+  const int32_t* table = a.table + (int64_t)k.S.seq * a.width;
+  bool bad = k.bad;
   auto record = [&](int p) -> const uint8_t* {
     int id = table[p];
     if (id < 0 || id >= a.pages) bad = true, id = 0;
-    return a.cache + ((int64_t)id * a.kv_heads + kh) * kRec;
+    return a.cache + ((int64_t)id * a.kv_heads + k.kh) * kRec;
   };
   auto load_k = [&](const uint8_t* rec) {
 #pragma unroll
@@ -228,161 +317,164 @@ __global__ __launch_bounds__(256) void kv4_attention_kernel(Kv4Args a, Kv4Batch 
 #pragma unroll
     for (int i = 0; i < 4; ++i) vs[i] = *reinterpret_cast<const u32x4*>(rec + kOffVs + 64 * q4 + 16 * i);
   };
-  // eight e2m1 codes times a scale as bf16 (exact)
-  auto widen = [](uint32_t x, float scale) {
-    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-    bf16x2 y[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 0), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 1),
-                   __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 2), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 3)};
-    return bf16x8{y[0][0], y[0][1], y[1][0], y[1][1], y[2][0], y[2][1], y[3][0], y[3][1]};
-  };
-  int p = p0 + w;
+  int p = k.p0 + w;
   const uint8_t* rec = nullptr;
-  if (p < p1) {
+  if (p < k.p1) {
     rec = record(p);
     load_k(rec);
     load_v(rec);
   }
-  for (; p < p1; p += 4) {
-    const bool more = p + 4 < p1;
+  for (; p < k.p1; p += 4) {
+    const bool more = p + 4 < k.p1;
     const uint8_t* next = more ? record(p + 4) : rec;
-    f32x4 st[RT][8];  // S^T[16 i + 4 q4 + r][row]
+    f32x4 st[8];  // S^T[16 i + 4 q4 + r][row]
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-#pragma unroll
-      for (int c = 0; c < RT; ++c) st[c][i] = f32x4{0, 0, 0, 0};
+      st[i] = f32x4{0, 0, 0, 0};
       const float sc = __uint_as_float(((i < 4 ? ks.x : ks.y) >> (8 * (i & 3)) & 255u) << 23);
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        const bf16x8 ak = widen(kr[i][s], sc);
-#pragma unroll
-        for (int c = 0; c < RT; ++c) st[c][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ak, qf[c][s], st[c][i], 0, 0, 0);
-      }
+      for (int s = 0; s < 4; ++s) st[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(kr[i][s], sc), qf[s], st[i], 0, 0, 0);
     }
     if (more) load_k(next);
-    const int t0 = p * kPage + 4 * q4;  // the lane's tokens: t0 + 16 i + r
-    bf16x8 pw[RT][4];
-    auto softmax = [&](auto masked) {
-#pragma unroll
-      for (int c = 0; c < RT; ++c) {
-        float mx = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            float v = st[c][i][r] * sl;
-            if constexpr (decltype(masked)::value) v = t0 + 16 * i + r <= lim[c] ? v : -INFINITY;
-            st[c][i][r] = v;
-            mx = fmaxf(mx, v);
-          }
-        mx = rows_max(mx);
-        if (__any(mx > m[c] + 8.0f)) {
-          const float mn = mx > m[c] + 8.0f ? mx : m[c];  // per row: no other row of the tile changes it
-          const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[c] - mn);
-          m[c] = mn;
-          l[c] *= alpha;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) o[c][j] *= alpha;
-        }
-        const float ms = m[c] == -INFINITY ? 0.0f : m[c];
-        float sum = 0.0f;
-        u32x4 pk[4];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          float x[4];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float e = __builtin_amdgcn_exp2f(st[c][i][r] - ms);
-            sum += e;
-            const float scale = bf16_bits_to_f32(vs[i >> 1][(i & 1) * 2 + (r >> 1)] >> (r & 1 ? 16 : 0) & 0xFFFFu);
-            x[r] = e * scale;
-            // places that no token was written to hold any bits
-            if constexpr (decltype(masked)::value) x[r] = t0 + 16 * i + r <= lim[c] ? x[r] : 0.0f;
-          }
-          pk[i >> 1][(i & 1) * 2] = pack_bf16x2(x[0], x[1]);
-          pk[i >> 1][(i & 1) * 2 + 1] = pack_bf16x2(x[2], x[3]);
-        }
-        l[c] += sum;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) pw[c][u] = __builtin_bit_cast(bf16x8, pk[u]);
-      }
-    };
+    bf16x8 pw[4];
     if ((int64_t)p * kPage + kPage - 1 <= all_see)
-      softmax(std::false_type{});
+      weigh<8, false>(st, pw, vs, sl, p * kPage + 4 * q4, lim, m, l, o);
     else
-      softmax(std::true_type{});
+      weigh<8, true>(st, pw, vs, sl, p * kPage + 4 * q4, lim, m, l, o);
 #pragma unroll
     for (int j = 0; j < 8; ++j)
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const bf16x8 av = widen(vr[j][u], 1.0f);
-#pragma unroll
-        for (int c = 0; c < RT; ++c) o[c][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, pw[c][u], o[c][j], 0, 0, 0);
-      }
+      for (int u = 0; u < 4; ++u) o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(vr[j][u], 1.0f), pw[u], o[j], 0, 0, 0);
     if (more) load_v(next);
     rec = next;
   }
   // the four waves' maxima, sums and O: waves 2 and 3 hand over to 0 and 1, then 1 to 0
-  extern __shared__ __align__(16) uint8_t smem[];  // two waves' O, then their (m, l)
-  f32x4* ex = reinterpret_cast<f32x4*>(smem);
-  float2* ml = reinterpret_cast<float2*>(smem + 2 * (size_t)RT * 8 * 64 * sizeof(f32x4));
-#pragma unroll
-  for (int c = 0; c < RT; ++c) {
-    l[c] = rows_sum(l[c]);
-    if (bad) l[c] = __uint_as_float(0x7FC00000u);
-  }
+  __shared__ f32x4 ex[2][8][64];
+  __shared__ float2 ml[2][64];
+  l = rows_sum(l);
+  if (bad) l = __uint_as_float(0x7FC00000u);
 #pragma unroll
   for (int step = 2; step > 0; step >>= 1) {
     __syncthreads();
     if (w >= step && w < 2 * step) {
+      ml[w - step][lane] = make_float2(m, l);
 #pragma unroll
-      for (int c = 0; c < RT; ++c) {
-        ml[((w - step) * RT + c) * 64 + lane] = make_float2(m[c], l[c]);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) ex[(((w - step) * RT + c) * 8 + j) * 64 + lane] = o[c][j];
-      }
+      for (int j = 0; j < 8; ++j) ex[w - step][j][lane] = o[j];
     }
     __syncthreads();
     if (w < step) {
+      const float2 other = ml[w][lane];
+      const float mn = fmaxf(m, other.x), ms = mn == -INFINITY ? 0.0f : mn;
+      const float fa = __builtin_amdgcn_exp2f(m - ms), fb = __builtin_amdgcn_exp2f(other.x - ms);
+      m = mn;
+      l = l * fa + other.y * fb;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o[j] = o[j] * fa + ex[w][j][lane] * fb;
+    }
+  }
+  if (w == 0) write_rows(a, k, l16, m, l, o, q4);
+}
+
+// Attention of 64 RT query rows per workgroup (prompts in chunks): every wave owns RT tiles of 16 rows and goes over all
+// pages of the split, which lie in LDS as they are in the cache, the next one on its way. Nothing is joined between the waves.
+template <int RT>
+__global__ __launch_bounds__(256, 2) void kv4_chunk_kernel(Kv4Args a, Kv4Batch b) {
+  constexpr int PT = 4;  // tiles of 16 tokens whose scores are held at a time
+  Kv4Work k;
+  if (k.locate(a, b)) return;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l16 = lane & 15, q4 = lane >> 4;
+  extern __shared__ __align__(16) uint8_t smem[];  // two pages
+  const int row0 = k.rb * 64 * RT + 16 * RT * w;   // the wave's first row
+  const bool rows = row0 < k.S.n * k.g;
+  bf16x8 qf[RT][4];
+  int lim[RT];
+  float m[RT], l[RT];
+  f32x4 o[RT][8];
+#pragma unroll
+  for (int c = 0; c < RT; ++c) {
+    lim[c] = load_rows(qf[c], a, k, row0 + 16 * c + l16, q4);
+    m[c] = -INFINITY, l[c] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[c][j] = f32x4{0, 0, 0, 0};
+  }
+  const int64_t all_see = k.first + row0 / k.g;  // every row of the wave sees the positions up to here
+  const int64_t none_see = k.first + min(row0 + 16 * RT - 1, k.S.n * k.g - 1) / k.g;  // and none those behind this
+  const float sl = a.scale * kLog2e;
+  const int32_t* table = a.table + (int64_t)k.S.seq * a.width;
+  bool bad = k.bad;
+  // Page p to LDS without registers, 1 KiB a load; the last is 768 bytes and zeros.
+  auto load = [&](int p) {
+    int id = table[p];
+    if (id < 0 || id >= a.pages) bad = true, id = 0;
+    const __amdgpu_buffer_rsrc_t r = buffer_rsrc(a.cache + ((int64_t)id * a.kv_heads + k.kh) * kRec, kRec);
+    uint8_t* dst = smem + (p & 1) * kChunkBuf;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(dst + i * 4096 + w * 1024), 16,
+                                               i * 4096 + w * 1024 + lane * 16, 0, 0, 0);
+    if (w == 0)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(dst + kOffKs), 16, kOffKs + lane * 16, 0, 0, 0);
+  };
+  if (k.p0 < k.p1) load(k.p0);
+  for (int p = k.p0; p < k.p1; ++p) {
+    // This wave's loads have landed; then every wave's have, and every wave is done with the other buffer.
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    if (p + 1 < k.p1) load(p + 1);
+    const uint8_t* rec = smem + (p & 1) * kChunkBuf;
+    if (!rows || (int64_t)p * kPage > none_see) continue;
+    const bool whole = (int64_t)p * kPage + kPage - 1 <= all_see;
+    const uint2 ks = *reinterpret_cast<const uint2*>(rec + kOffKs + 128 * q4 + 8 * l16);
+#pragma unroll
+    for (int h0 = 0; h0 < 8; h0 += PT) {
+      f32x4 st[RT][PT];  // S^T[16 (h0 + i) + 4 q4 + r][row]
+#pragma unroll
+      for (int i = 0; i < PT; ++i) {
+        const u32x4 kr = *reinterpret_cast<const u32x4*>(rec + (16 * (h0 + i) + l16) * 64 + 16 * q4);
+        const float sc = __uint_as_float(((h0 + i < 4 ? ks.x : ks.y) >> (8 * ((h0 + i) & 3)) & 255u) << 23);
+#pragma unroll
+        for (int c = 0; c < RT; ++c) st[c][i] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+          const bf16x8 ak = widen(kr[s], sc);
+#pragma unroll
+          for (int c = 0; c < RT; ++c) st[c][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ak, qf[c][s], st[c][i], 0, 0, 0);
+        }
+      }
+      u32x4 vs[PT / 2];
+#pragma unroll
+      for (int i = 0; i < PT / 2; ++i) vs[i] = *reinterpret_cast<const u32x4*>(rec + kOffVs + 64 * q4 + 8 * h0 + 16 * i);
+      bf16x8 pw[RT][PT / 2];
+      const int t0 = p * kPage + 16 * h0 + 4 * q4;
 #pragma unroll
       for (int c = 0; c < RT; ++c) {
-        const float2 other = ml[(w * RT + c) * 64 + lane];
-        const float mn = fmaxf(m[c], other.x), ms = mn == -INFINITY ? 0.0f : mn;
-        const float fa = __builtin_amdgcn_exp2f(m[c] - ms), fb = __builtin_amdgcn_exp2f(other.x - ms);
-        m[c] = mn;
-        l[c] = l[c] * fa + other.y * fb;
+        if (whole)
+          weigh<PT, false>(st[c], pw[c], vs, sl, t0, lim[c], m[c], l[c], o[c]);
+        else
+          weigh<PT, true>(st[c], pw[c], vs, sl, t0, lim[c], m[c], l[c], o[c]);
+      }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) o[c][j] = o[c][j] * fa + ex[((w * RT + c) * 8 + j) * 64 + lane] * fb;
+      for (int j = 0; j < 8; ++j) {
+        const uint2 vr = *reinterpret_cast<const uint2*>(rec + kOffV + (16 * j + l16) * 64 + 16 * q4 + 2 * h0);
+#pragma unroll
+        for (int u = 0; u < PT / 2; ++u) {
+          const bf16x8 av = widen(u ? vr.y : vr.x, 1.0f);
+#pragma unroll
+          for (int c = 0; c < RT; ++c) o[c][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, pw[c][u], o[c][j], 0, 0, 0);
+        }
       }
     }
   }
-  if (w != 0) return;
-  const int64_t unit = ((int64_t)(S.blk0 + rb) * a.kv_heads + kh) * a.splits + split;
+  if (!rows) return;
 #pragma unroll
-  for (int c = 0; c < RT; ++c) {
-    const int row = rb * R + 16 * c + l16, i = row / g, j0 = row % g;
-    if (row >= S.n * g) continue;
-    if (a.splits > 1) {
-      float* po = a.part + (unit * R + 16 * c + l16) * DH;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) *reinterpret_cast<f32x4*>(po + 16 * j + 4 * q4) = o[c][j];
-      if (q4 == 0) a.part_ml[unit * R + 16 * c + l16] = make_float2(m[c], l[c]);
-      continue;
-    }
-    const int64_t at = (S.row0 + i) * a.heads + kh * g + j0;
-    const float inv = l[c] == 0.0f ? 0.0f : 1.0f / l[c];  // a row that sees nothing: 0, lse -inf
-    if (q4 == 0) a.lse[(int64_t)(kh * g + j0) * a.N + S.row0 + i] = l[c] == 0.0f ? -INFINITY : m[c] / kLog2e + logf(l[c]);
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      *reinterpret_cast<uint2*>(a.o + at * DH + 16 * j + 4 * q4) =
-          make_uint2(pack_bf16x2(o[c][j][0] * inv, o[c][j][1] * inv), pack_bf16x2(o[c][j][2] * inv, o[c][j][3] * inv));
-  }
+  for (int c = 0; c < RT; ++c)
+    write_rows(a, k, 16 * RT * w + 16 * c + l16, m[c], bad ? __uint_as_float(0x7FC00000u) : rows_sum(l[c]), o[c], q4);
 }
 
 // Joins the splits of a row in their order. One wave per (row, query head), two elements a lane.
-template <int RT>
 __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Args a, Kv4Batch b, int64_t rows) {
-  constexpr int R = 16 * RT;
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, R = a.block_rows;
   const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);  // (row of the batch, head)
   if (at >= rows * a.heads) return;
   const int64_t row = b.s[0].row0 + at / a.heads;
@@ -427,14 +519,14 @@ hipError_t launch_kv4_append(const Kv4Args& a, Kv4Batch b, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <int RT>
-static hipError_t launch_rows(LdsLimit& limit, const Kv4Args& a, Kv4Batch b, hipStream_t s) {
-  constexpr size_t lds = 2 * (size_t)RT * 8 * 64 * sizeof(f32x4) + 2 * (size_t)RT * 64 * sizeof(float2);
-  if (hipError_t e = limit.raise((const void*)kv4_attention_kernel<RT>, lds)) return e;
+template <class K>
+static hipError_t launch_blocks(K kernel, LdsLimit& limit, size_t lds, const Kv4Args& a, Kv4Batch b, hipStream_t s) {
+  if (lds)
+    if (hipError_t e = limit.raise((const void*)kernel, lds)) return e;
   const int g = a.heads / a.kv_heads;
   int64_t n = 0, rows = 0;
   for (int i = 0; i < b.count; ++i) {
-    const int64_t blocks = ((int64_t)b.s[i].n * g + 16 * RT - 1) / (16 * RT);
+    const int64_t blocks = ((int64_t)b.s[i].n * g + a.block_rows - 1) / a.block_rows;
     b.s[i].wg_begin = (int32_t)n;
     n += blocks * a.kv_heads * a.splits;
     rows += b.s[i].n;
@@ -442,20 +534,20 @@ static hipError_t launch_rows(LdsLimit& limit, const Kv4Args& a, Kv4Batch b, hip
   if (n <= 0) return hipSuccess;
   {
     KernelTimer t(K_KV4_ATTN, s);
-    hipLaunchKernelGGL(kv4_attention_kernel<RT>, dim3((unsigned)n), dim3(256), lds, s, a, b);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)n), dim3(256), lds, s, a, b);
   }
   if (a.splits > 1) {
     KernelTimer t(K_KV4_JOIN, s);
-    hipLaunchKernelGGL(kv4_join_kernel<RT>, dim3((unsigned)((rows * a.heads + 3) / 4)), dim3(256), 0, s, a, b, rows);
+    hipLaunchKernelGGL(kv4_join_kernel, dim3((unsigned)((rows * a.heads + 3) / 4)), dim3(256), 0, s, a, b, rows);
   }
   return hipGetLastError();
 }
 
-hipError_t launch_kv4_attention(int row_tiles, const Kv4Args& a, const Kv4Batch& b, hipStream_t s) {
+hipError_t launch_kv4_attention(const Kv4Args& a, const Kv4Batch& b, hipStream_t s) {
   static LdsLimit limits[3];
-  return row_tiles == 1   ? launch_rows<1>(limits[0], a, b, s)
-         : row_tiles == 2 ? launch_rows<2>(limits[1], a, b, s)
-                          : launch_rows<4>(limits[2], a, b, s);
+  return a.block_rows == 16   ? launch_blocks(kv4_decode_kernel, limits[0], 0, a, b, s)
+         : a.block_rows == 64 ? launch_blocks(kv4_chunk_kernel<1>, limits[1], 2 * kChunkBuf, a, b, s)
+                              : launch_blocks(kv4_chunk_kernel<2>, limits[2], 2 * kChunkBuf, a, b, s);
 }
 
 }  // namespace attt
