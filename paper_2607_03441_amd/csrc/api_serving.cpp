@@ -82,8 +82,8 @@ Kv4Plan kv4_plan(const Rows& rows, int32_t E, int32_t heads, int32_t kv_heads, i
   P.block_rows = most <= 16 ? 16 : most <= 64 ? 64 : 128;
   for (int32_t e = 0; e < E; ++e) P.units += ceil_div(rows.count(e) * g, P.block_rows) * kv_heads;
   const int64_t pages = std::max<int64_t>(1, ceil_div(max_length, kKv4Page));
-  // Workgroups of 16 rows take four pages at a time, one a wave, the others one.
-  const int64_t step = P.block_rows == 16 ? 4 : 1, wanted = P.block_rows == 16 ? 1024 : 512;
+  // Workgroups of 16 rows take four pages at a time, one a wave: eight at least, so that each has one on its way.
+  const int64_t step = P.block_rows == 16 ? 8 : 1, wanted = P.block_rows == 16 ? 2048 : 1024;
   const int64_t chunk = std::max(step, round_up(ceil_div(pages * P.units, wanted), step));
   P.chunk = (int32_t)std::min(chunk, round_up(pages, step));
   P.splits = (int32_t)ceil_div(pages, P.chunk);
@@ -101,6 +101,9 @@ Kv4Batch kv4_batch(const Rows& rows, int32_t e0, int32_t E, int64_t group, int32
     b.s[i].blk0 = (int32_t)blk0;
     blk0 += ceil_div(rows.count(e0 + i) * group, block_rows);
   }
+  b.same = b.s[0].n;
+  for (int i = 1; i < b.count; ++i)
+    if (b.s[i].n != b.same) b.same = 0;
   return b;
 }
 

@@ -224,7 +224,8 @@ struct Kv4Seq {
 };
 struct Kv4Batch {
   int32_t count;
-  int32_t pad;
+  int32_t same;         // rows of every sequence where all have as many, else 0
+  int32_t wgs, blocks;  // workgroups and row blocks of the first sequence (set at launch)
   Kv4Seq s[kEpBatch];
 };
 hipError_t launch_kv4_append(const Kv4Args& a, Kv4Batch b, hipStream_t s);

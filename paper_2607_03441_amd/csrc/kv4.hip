@@ -13,6 +13,8 @@
 //           One scale per token (bf16 with 6 significant bits), in the same order: it goes into the
 //           weight, because the contraction runs over the tokens.
 // Codes times scales have at most 8 significant bits, so the bf16 operands of the products are exact.
+#include <type_traits>
+
 #include "common.hpp"
 #include "internal.hpp"
 #include "lds_limit.hpp"
@@ -27,49 +29,59 @@ static_assert(kOffVs + kPage * 2 == kRec, "the record's parts");
 constexpr size_t kChunkBuf = kOffKs + 1024;  // a page in LDS
 constexpr float kLog2e = 1.4426950408889634f;
 
-// Where token t of a page stands in a value row.
-__device__ __forceinline__ int value_pos(int t) { return 32 * ((t >> 2) & 3) + 4 * (t >> 4) + (t & 3); }
-
-// Sequence of workgroup `bid`: the last whose wg_begin is at most bid.
-__device__ __forceinline__ int find_seq(const Kv4Batch& b, int bid) {
+// Sequence of workgroup `bid`: the last whose wg_begin is at most bid. Where all have the same rows (decoding), none of
+// the batch's entries needs to be read for it.
+__device__ __forceinline__ Kv4Seq find_seq(const Kv4Batch& b, int bid) {
+  if (b.same) {
+    const int e = bid / b.wgs;
+    return {b.s[0].row0 + (int64_t)e * b.same, b.same, b.s[0].seq + e, e * b.wgs, b.s[0].blk0 + e * b.blocks};
+  }
   const int lane = threadIdx.x & 63;
-  return __builtin_amdgcn_readfirstlane(__popcll(__ballot(lane < b.count && b.s[lane < b.count ? lane : 0].wg_begin <= bid)) - 1);
+  return b.s[__builtin_amdgcn_readfirstlane(__popcll(__ballot(lane < b.count && b.s[lane < b.count ? lane : 0].wg_begin <= bid)) - 1)];
 }
 
-// e2m1 code of x: to nearest, ties to the even code, 6 at most; the sign of a zero is kept.
-__device__ __forceinline__ uint32_t e2m1(float x) {
-  const float a = fabsf(x);
-  const uint32_t mag = (a > 0.25f) + (a >= 0.75f) + (a > 1.25f) + (a >= 1.75f) + (a > 2.5f) + (a >= 3.5f) + (a > 5.0f);
-  return mag | (__float_as_uint(x) >> 28 & 8u);
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+  return v;
 }
-__device__ __forceinline__ float e2m1_value(uint32_t c) {
-  const uint32_t m = c & 7u;
-  const float v = m < 4u ? 0.5f * (float)m : m == 4u ? 2.0f : m == 5u ? 3.0f : m == 6u ? 4.0f : 6.0f;
-  return c & 8u ? -v : v;
+
+// eight e2m1 codes times a scale as bf16 (exact)
+__device__ __forceinline__ bf16x8 widen(uint32_t x, float scale) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const bf16x2 y[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 0), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 1),
+                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 2), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 3)};
+  return bf16x8{y[0][0], y[0][1], y[1][0], y[1][1], y[2][0], y[2][1], y[3][0], y[3][1]};
 }
 }  // namespace
 
-// The new rows of one (sequence, key/value head) that fall into one page. Sixteen lanes take a token, eight
-// elements each: the maxima of its key blocks (4 lanes) and of its value row (16 lanes) meet in shuffles. Key codes go
-// to the page at once; value codes are turned through LDS, and each 16-byte piece of a value row is
-// written by one thread, which keeps the codes of the tokens that were there.
+// The new rows of one (sequence, key/value head) that fall into one page and there onto the tokens 16 i + 4 q + r of one q:
+// those 32 make up one 16-byte piece of every value row, so no two workgroups write into one piece. Sixteen lanes take a
+// token, eight elements each, two tokens after the other with both loads on their way: the maxima of its key blocks
+// (4 lanes) and of its value row (16 lanes) meet in shuffles. Key codes go to the page at once; value codes are
+// turned through LDS, and each piece is written by one thread, which keeps the codes of the tokens that were there.
+// (A workgroup per page, 16 tokens at a time, took 44 us for 16 x 512 rows of 8 heads.)
 __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Args a, Kv4Batch b) {
-  const Kv4Seq S = b.s[find_seq(b, blockIdx.x)];
+  const Kv4Seq S = find_seq(b, blockIdx.x);
   const int local = (int)blockIdx.x - S.wg_begin;
-  const int kh = local % a.kv_heads;
+  // the four pieces of a page and head eight workgroups apart, on one XCD, whose L2 puts their writes into whole lines
+  const int q = local >> 3 & 3, unit = (local >> 5) * 8 + (local & 7), kh = unit % a.kv_heads, nth = unit / a.kv_heads;
+  const int lane16 = threadIdx.x & 15;
+  u32x4 xk[2], xv[2];
+  if (S.n == 1) {  // the one row is known before the length is
+    const int64_t at = (S.row0 * a.kv_heads + kh) * DH + lane16 * 8;
+    xk[0] = xk[1] = *reinterpret_cast<const u32x4*>(a.k + at);
+    xv[0] = xv[1] = *reinterpret_cast<const u32x4*>(a.v + at);
+  }
   const int64_t len = a.lengths[S.seq];
   const int64_t first = len - S.n;  // position of the sequence's first new row; rows before 0 are not stored
-  const int64_t page = (first > 0 ? first : 0) / kPage + local / a.kv_heads;
+  const int64_t page = (first > 0 ? first : 0) / kPage + nth;
   const bool bad_len = len > a.width * kPage;
-  const int id = page < a.width && !bad_len && page * kPage < len ? a.table[S.seq * a.width + page] : -1;
-  const bool stored = id >= 0 && id < a.pages;
-  __shared__ __align__(16) uint8_t codes[DH][kPage + 16];  // value codes by (element, position); pitch 144
-  const int tid = threadIdx.x, lane16 = tid & 15;
+  __shared__ __align__(16) uint8_t codes[DH][32 + 16];  // value codes by (element, place in the piece)
+  const int tid = threadIdx.x;
   const bool held = a.k_held != nullptr;
-  uint8_t* rec = a.cache + ((int64_t)(stored ? id : 0) * a.kv_heads + kh) * kRec;
-  // rows [i0, i1) of the sequence lie in this page
-  const int i0 = (int)max((int64_t)0, page * kPage - first), i1 = (int)min((int64_t)S.n, page * kPage + kPage - first);
-  if (local / a.kv_heads == 0 && held) {
+  if (nth >= (S.n + kPage - 2) / kPage + 1) return;
+  if (nth == 0 && q == 0 && held) {
     // what the sequence has no place for: rows before its start hold nothing, those of a bad length NaN
     const int none = bad_len ? S.n : (int)min((int64_t)S.n, max((int64_t)0, -first));
     const uint32_t fill = bad_len ? 0x7FC07FC0u : 0u;
@@ -79,19 +91,41 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Args a, Kv4Batch b) 
       *reinterpret_cast<u32x4*>(a.v_held + at) = u32x4{fill, fill, fill, fill};
     }
   }
-  if (bad_len || i0 >= i1) return;
-  for (int i = i0 + (tid >> 4); i - (tid >> 4) < i1; i += 16) {
-    const bool on = i < i1;
-    const int64_t at = ((S.row0 + (on ? i : i0)) * a.kv_heads + kh) * DH + lane16 * 8;
-    const u32x4 xk = *reinterpret_cast<const u32x4*>(a.k + at), xv = *reinterpret_cast<const u32x4*>(a.v + at);
-    float fk[8], fv[8];
+  // tokens [t0, t1) of the page are new
+  const int t0 = (int)max((int64_t)0, max((int64_t)0, first) - page * kPage), t1 = (int)min((int64_t)kPage, len - page * kPage);
+  // a run of tokens touches pieces t0 / 4, t0 / 4 + 1, ... in turn
+  if (bad_len || t0 >= t1 || ((q - (t0 >> 2)) & 3) > ((t1 - 1) >> 2) - (t0 >> 2)) return;
+  // this thread's tokens: places 16 u + tid / 16 of the piece, 4 i + r of token 16 i + 4 q + r
+  int t[2];
+  bool on[2];
+  int64_t at[2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int place = 16 * u + (tid >> 4);
+    t[u] = 16 * (place >> 2) + 4 * q + (place & 3);
+    on[u] = t[u] >= t0 && t[u] < t1;
+    at[u] = ((S.row0 + (on[u] ? page * kPage + t[u] - first : 0)) * a.kv_heads + kh) * DH + lane16 * 8;
+  }
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    if (S.n == 1) break;
+    xk[u] = *reinterpret_cast<const u32x4*>(a.k + at[u]);
+    xv[u] = *reinterpret_cast<const u32x4*>(a.v + at[u]);
+  }
+  const int id = a.table[S.seq * a.width + page];
+  const bool stored = id >= 0 && id < a.pages;
+  uint8_t* rec = a.cache + ((int64_t)(stored ? id : 0) * a.kv_heads + kh) * kRec;
+  u32x4* piece = reinterpret_cast<u32x4*>(rec + kOffV + (tid & (DH - 1)) * 64 + q * 16);
+  u32x4 was = u32x4{0, 0, 0, 0};
+  if (stored && tid < DH && t1 - t0 < kPage) was = *piece;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    if (!__any(on[u])) continue;
     uint32_t mk = 0, mv = 0;  // the largest magnitude, as bits: NaN above infinity above the rest
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      fk[e] = bf16_bits_to_f32(xk[e >> 1] >> (e & 1 ? 16 : 0) & 0xFFFFu);
-      fv[e] = bf16_bits_to_f32(xv[e >> 1] >> (e & 1 ? 16 : 0) & 0xFFFFu);
-      mk = max(mk, __float_as_uint(fk[e]) & 0x7FFFFFFFu);
-      mv = max(mv, __float_as_uint(fv[e]) & 0x7FFFFFFFu);
+    for (int e = 0; e < 4; ++e) {
+      mk = max(mk, max(xk[u][e] << 16 & 0x7FFF0000u, xk[u][e] & 0x7FFF0000u));
+      mv = max(mv, max(xv[u][e] << 16 & 0x7FFF0000u, xv[u][e] & 0x7FFF0000u));
     }
 #pragma unroll
     for (int o = 1; o < 16; o <<= 1) {
@@ -102,76 +136,80 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Args a, Kv4Batch b) 
     // times half of it): the exponent, less 2, rounded up from 1.75; at least 2^-100, and 6 times it is finite.
     const bool nan_k = mk >= 0x7F800000u, nan_v = mv >= 0x7F800000u;
     const uint32_t ek = nan_k ? 255u : min(252, max(27, (int)((mk + 0x200000u) >> 23) - 2));
-    const float ik = __uint_as_float((254u - min(ek, 253u)) << 23);  // 2^(127 - ek), exact
+    const float sk = __uint_as_float((nan_k ? 127u : ek) << 23);
     // values: a sixth of the largest, rounded up to 6 significant bits, so that the largest is 6 at most
     // (bounded like the keys')
-    const float sixth = __fdiv_rn(__uint_as_float(mv), 6.0f);
-    const float sv = nan_v ? __uint_as_float(0x7FC00000u)
-                           : fminf(fmaxf(__uint_as_float((__float_as_uint(sixth) + 0x3FFFFu) & ~0x3FFFFu), 0x1p-100f), 0x1.5p125f);
-    const int t = (int)(first + i - page * kPage);  // in the page
-    uint32_t ck[8], cv[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      ck[e] = nan_k ? 0u : e2m1(fk[e] * ik);
-      cv[e] = nan_v ? 0u : e2m1(__fdiv_rn(fv[e], sv));
+    const float sixth = __fdiv_rn(nan_v ? 1.0f : __uint_as_float(mv), 6.0f);
+    const float sv = fminf(fmaxf(__uint_as_float((__float_as_uint(sixth) + 0x3FFFFu) & ~0x3FFFFu), 0x1p-100f), 0x1.5p125f);
+    // The matrix core's own conversions round to nearest, ties to the even code, and stop at 6. A value over its scale
+    // is first rounded to float32, with one correction of the product with the reciprocal: a quotient that lies
+    // on the border of two codes is exact then, and any other is at least 2^-9 of itself away from one.
+    const float rv = __fdiv_rn(1.0f, sv);
+    uint32_t wk = 0, wv = 0;
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    auto pair = [&](uint32_t x, auto sel) {
+      const float lo = bf16_bits_to_f32(x & 0xFFFFu), hi = __uint_as_float(x & 0xFFFF0000u);
+      auto over = [&](float x) {
+        const float y = x * rv;
+        return copysignf(fmaf(fmaf(-y, sv, x), rv, y), x);  // a zero keeps its sign
+      };
+      wv = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(wv, over(lo), over(hi), 1.0f, decltype(sel)::value);
+    };
+    auto pair_k = [&](uint32_t x, auto sel) {
+      wk = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(wk, bf16_bits_to_f32(x & 0xFFFFu), __uint_as_float(x & 0xFFFF0000u), sk,
+                                                    decltype(sel)::value);
+    };
+    pair_k(xk[u][0], std::integral_constant<int, 0>{}), pair(xv[u][0], std::integral_constant<int, 0>{});
+    pair_k(xk[u][1], std::integral_constant<int, 1>{}), pair(xv[u][1], std::integral_constant<int, 1>{});
+    pair_k(xk[u][2], std::integral_constant<int, 2>{}), pair(xv[u][2], std::integral_constant<int, 2>{});
+    pair_k(xk[u][3], std::integral_constant<int, 3>{}), pair(xv[u][3], std::integral_constant<int, 3>{});
+    if (nan_k) wk = 0;
+    if (nan_v) wv = 0;
+    const int place = 16 * u + (tid >> 4);
+    if (on[u] && stored) {
+      *reinterpret_cast<uint32_t*>(rec + t[u] * 64 + lane16 * 4) = wk;
+      if ((lane16 & 3) == 0) rec[kOffKs + (lane16 >> 2) * 128 + (t[u] & 15) * 8 + (t[u] >> 4)] = (uint8_t)ek;
+      if (lane16 == 0)
+        *reinterpret_cast<uint16_t*>(rec + kOffVs + 2 * (32 * q + place)) = nan_v ? 0x7FC0 : (uint16_t)(__float_as_uint(sv) >> 16);
     }
-    if (on && stored) {
-      uint32_t w = 0;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) w |= ck[e] << (4 * e);
-      *reinterpret_cast<uint32_t*>(rec + t * 64 + lane16 * 4) = w;
-      if ((lane16 & 3) == 0) rec[kOffKs + (lane16 >> 2) * 128 + (t & 15) * 8 + (t >> 4)] = (uint8_t)ek;
-      const int p = value_pos(t);
-      if (lane16 == 0) *reinterpret_cast<uint16_t*>(rec + kOffVs + 2 * p) = (uint16_t)(__float_as_uint(sv) >> 16);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) codes[lane16 * 8 + e][p] = (uint8_t)cv[e];
-    }
-    if (on && held) {
-      const float sk = nan_k ? __uint_as_float(0x7FC00000u) : __uint_as_float(ek << 23);
-      const float pv = stored ? sv : __uint_as_float(0x7FC00000u), pk = stored ? sk : __uint_as_float(0x7FC00000u);
-      u32x4 hk, hv;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        hk[e] = pack_bf16x2(e2m1_value(ck[2 * e]) * pk, e2m1_value(ck[2 * e + 1]) * pk);
-        hv[e] = pack_bf16x2(e2m1_value(cv[2 * e]) * pv, e2m1_value(cv[2 * e + 1]) * pv);
-      }
-      *reinterpret_cast<u32x4*>(a.k_held + at) = hk;
-      *reinterpret_cast<u32x4*>(a.v_held + at) = hv;
+    for (int e = 0; e < 8; ++e) codes[lane16 * 8 + e][place] = (uint8_t)(wv >> (4 * e) & 15u);
+    if (on[u] && held) {
+      u32x4 hk = __builtin_bit_cast(u32x4, widen(wk, sk)), hv;
+      auto value = [&](int e, auto sel) {
+        const f32x2 y = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(wv, 1.0f, decltype(sel)::value);
+        hv[e] = pack_bf16x2(y[0] * sv, y[1] * sv);
+      };
+      value(0, std::integral_constant<int, 0>{}), value(1, std::integral_constant<int, 1>{});
+      value(2, std::integral_constant<int, 2>{}), value(3, std::integral_constant<int, 3>{});
+      const u32x4 nan = u32x4{0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u};
+      *reinterpret_cast<u32x4*>(a.k_held + at[u]) = nan_k || !stored ? nan : hk;
+      *reinterpret_cast<u32x4*>(a.v_held + at[u]) = nan_v || !stored ? nan : hv;
     }
   }
-  if (!stored) return;
   __syncthreads();
-  const int t0 = (int)(first + i0 - page * kPage), t1 = (int)(first + i1 - page * kPage);  // tokens [t0, t1) are new
-  for (int j = tid; j < DH * 4; j += 256) {
-    const int d = j >> 2, q = j & 3;  // positions 32 q .. +31: tokens 16 i + 4 q + r
-    u32x4* dst = reinterpret_cast<u32x4*>(rec + kOffV + d * 64 + q * 16);
-    u32x4 keep = u32x4{0, 0, 0, 0}, w = u32x4{0, 0, 0, 0};
+  if (!stored || tid >= DH) return;
+  u32x4 w, keep = u32x4{0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+  for (int half = 0; half < 2; ++half) {  // 16 codes, a byte each, become 8 bytes
+    const u32x4 x = *reinterpret_cast<const u32x4*>(&codes[tid][16 * half]);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int t = 16 * i + 4 * q + r, s = 16 * (i & 1) + 4 * r;
-        if (t >= t0 && t < t1)
-          w[i >> 1] |= (uint32_t)codes[d][32 * q + 4 * i + r] << s;
-        else
-          keep[i >> 1] |= 0xFu << s;
-      }
-    const bool all = (keep[0] | keep[1] | keep[2] | keep[3]) == 0u;
-    if ((keep[0] & keep[1] & keep[2] & keep[3]) == 0xFFFFFFFFu) continue;  // none of the new tokens
-    if (!all) w |= *dst & keep;
-    *dst = w;
+    for (int e = 0; e < 2; ++e) {
+      const uint32_t lo = x[2 * e] | x[2 * e] >> 4, hi = x[2 * e + 1] | x[2 * e + 1] >> 4;  // pairs in bytes 0 and 2
+      w[2 * half + e] = (lo & 0xFFu) | (lo >> 8 & 0xFF00u) | (hi & 0xFFu) << 16 | (hi << 8 & 0xFF000000u);
+    }
   }
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int tok = 16 * i + 4 * q + r;
+      if (tok < t0 || tok >= t1) keep[i >> 1] |= 0xFu << (16 * (i & 1) + 4 * r);
+    }
+  *piece = (w & ~keep) | (was & keep);
 }
 
 namespace {
-// eight e2m1 codes times a scale as bf16 (exact)
-__device__ __forceinline__ bf16x8 widen(uint32_t x, float scale) {
-  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-  const bf16x2 y[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 0), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 1),
-                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 2), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, 3)};
-  return bf16x8{y[0][0], y[0][1], y[1][0], y[1][1], y[2][0], y[2][1], y[3][0], y[3][1]};
-}
-
 // What a workgroup of the attention works on: rows rb R .. of a head's group (row i g + j: token i, query head j),
 // pages [p0, p1) of the sequence.
 struct Kv4Work {
@@ -181,7 +219,7 @@ struct Kv4Work {
   bool bad;       // a length beyond the bound: the rows are NaN
   // whether there is nothing to write either
   __device__ __forceinline__ bool locate(const Kv4Args& a, const Kv4Batch& b) {
-    S = b.s[find_seq(b, blockIdx.x)];
+    S = find_seq(b, blockIdx.x);
     const int local = (int)blockIdx.x - S.wg_begin;
     kh = local % a.kv_heads;
     const int sb = local / a.kv_heads;
@@ -480,8 +518,8 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Args a, Kv4Batch b, in
   const int64_t row = b.s[0].row0 + at / a.heads;
   const int h = (int)(at % a.heads), g = a.heads / a.kv_heads;
   // rows of empty sequences do not exist, so the last sequence that begins at or before the row holds it
-  const int e = __popcll(__ballot(lane < b.count && b.s[lane < b.count ? lane : 0].row0 <= row)) - 1;
-  const Kv4Seq S = b.s[e];
+  const Kv4Seq S = b.same ? find_seq(b, (int)(row - b.s[0].row0) / b.same * b.wgs)
+                          : b.s[__popcll(__ballot(lane < b.count && b.s[lane < b.count ? lane : 0].row0 <= row)) - 1];
   const int r = (int)(row - S.row0) * g + h % g;
   int64_t len = a.lengths[S.seq];
   if (len < 0 || len > a.max_length) len = 0;  // of a bad length the first split's sum is NaN
@@ -490,17 +528,28 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Args a, Kv4Batch b, in
   const int64_t unit = ((int64_t)(S.blk0 + r / R) * a.kv_heads + h / g) * a.splits;
   float m = -INFINITY, l = 0.0f;
   float2 o = make_float2(0.0f, 0.0f);
-#pragma unroll 4
-  for (int s = 0; s < ns; ++s) {
-    const int64_t u = (unit + s) * R + r % R;
-    const float2 ml = a.part_ml[u];
-    const float2 x = *reinterpret_cast<const float2*>(a.part + u * DH + 2 * lane);
-    const float mn = fmaxf(m, ml.x), ms = mn == -INFINITY ? 0.0f : mn;
-    const float fa = __builtin_amdgcn_exp2f(m - ms), fb = __builtin_amdgcn_exp2f(ml.x - ms);
+  for (int s0 = 0; s0 < ns; s0 += 64) {  // a lane's factor is that of split s0 + lane
+    const int n = __builtin_amdgcn_readfirstlane(min(64, ns - s0));
+    const int64_t u = (unit + s0) * R + r % R;
+    const float2 ml = lane < n ? a.part_ml[u + (int64_t)lane * R] : make_float2(-INFINITY, 0.0f);
+    const float mn = fmaxf(m, wave_max(ml.x)), ms = mn == -INFINITY ? 0.0f : mn;
+    const float f = __builtin_amdgcn_exp2f(ml.x - ms), fa = __builtin_amdgcn_exp2f(m - ms);
     m = mn;
-    l = l * fa + ml.y * fb;
-    o.x = o.x * fa + x.x * fb;
-    o.y = o.y * fa + x.y * fb;
+    l = l * fa + group_sum<64>(ml.y * f);
+    o.x *= fa;
+    o.y *= fa;
+    for (int s = 0; s < n; s += 8) {
+      float2 x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        x[i] = *reinterpret_cast<const float2*>(a.part + (u + (int64_t)min(s + i, n - 1) * R) * DH + 2 * lane);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {  // the factors of lanes past n are 0
+        const float fs = s + i < n ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s + i)) : 0.0f;
+        o.x = fmaf(x[i].x, fs, o.x);
+        o.y = fmaf(x[i].y, fs, o.y);
+      }
+    }
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   if (lane == 0) a.lse[(int64_t)h * a.N + row] = l == 0.0f ? -INFINITY : m / kLog2e + logf(l);
@@ -511,7 +560,8 @@ hipError_t launch_kv4_append(const Kv4Args& a, Kv4Batch b, hipStream_t s) {
   int64_t n = 0;
   for (int i = 0; i < b.count; ++i) {
     b.s[i].wg_begin = (int32_t)n;
-    if (b.s[i].n > 0) n += (int64_t)((b.s[i].n + kPage - 2) / kPage + 1) * a.kv_heads;
+    if (b.s[i].n > 0) n += ((int64_t)((b.s[i].n + kPage - 2) / kPage + 1) * a.kv_heads + 7) / 8 * 32;
+    if (i == 0) b.wgs = (int32_t)n;
   }
   if (n <= 0) return hipSuccess;
   KernelTimer t(K_KV4_APPEND, s);
@@ -529,6 +579,7 @@ static hipError_t launch_blocks(K kernel, LdsLimit& limit, size_t lds, const Kv4
     const int64_t blocks = ((int64_t)b.s[i].n * g + a.block_rows - 1) / a.block_rows;
     b.s[i].wg_begin = (int32_t)n;
     n += blocks * a.kv_heads * a.splits;
+    if (i == 0) b.wgs = (int32_t)n, b.blocks = (int32_t)blocks;
     rows += b.s[i].n;
   }
   if (n <= 0) return hipSuccess;
