@@ -168,7 +168,8 @@ attt_status attt_attention_bwd_split(const void* q, const void* k, const void* v
  *   dsum       device float32 [heads][N]: D = rowsum(dO * O) (written)
  *   workspace  as for attt_attention_bwd_split (attt_attention_workspace_size bytes; NULL with 0
  *              bytes: one workgroup per key block, as attt_attention_bwd)
- * D is formed from the O given, that is from its bf16 values. */
+ * D is formed from the O given, that is from its bf16 values, but for the first 128 rows of every episode, where it is
+ * computed as by attt_attention_bwd. */
 attt_status attt_attention_fwd(const void* q, const void* k, const void* v, const int64_t* row_offsets,
                                int32_t num_episodes, int64_t N, int32_t heads, int32_t kv_heads,
                                int32_t head_dim, float scale, void* o, float* lse, void* stream);

@@ -123,42 +123,42 @@ __global__ __launch_bounds__(512) void lp_logits_big_kernel(LpArgs a, int tiles_
   }
 }
 
-// The same in float32: 64 x 64 tiles on the float32 matrix instruction, K in steps of 32 through LDS.
+// The same in float32: 64 x 64 tiles on the float32 matrix instruction, K in steps of 64 through LDS, the next step's
+// loads on their way (steps of 32 took 15 us for 512 x 256 x 4096: as many more waits).
 __global__ __launch_bounds__(256) void lp_logits_f32_kernel(LpArgs a, int tiles_t) {
-  constexpr int T = 64, K = 32, P = K + 4;
-  __shared__ __align__(16) float lds[2][2][T * P];
+  constexpr int T = 64, K = 64, P = K + 4;
+  __shared__ __align__(16) float lds[2][T * P];
   const int t0 = (int)(blockIdx.x % tiles_t) * T, v0 = (int)(blockIdx.x / tiles_t) * T;
   const float* A = static_cast<const float*>(a.W) + (int64_t)v0 * a.d;
   const float* B = static_cast<const float*>(a.h) + (int64_t)(a.row0 + t0) * a.d;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int wm = wave >> 1, wn = wave & 1, l32 = lane & 31, hi = lane >> 5;
-  const int lr = tid >> 3, lk = (tid & 7) * 4;
+  const int lr = tid >> 4, lk = (tid & 15) * 4;
   f32x16 acc;
 #pragma unroll
   for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
-  f32x4 ra[2], rb[2];
+  f32x4 ra[4], rb[4];
   auto load = [&](int k0) {
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int row = lr + 32 * u;
+    for (int u = 0; u < 4; ++u) {
+      const int row = lr + 16 * u;
       const bool kin = k0 + lk < a.d;
       ra[u] = kin && v0 + row < a.V ? *reinterpret_cast<const f32x4*>(A + (int64_t)row * a.d + k0 + lk) : f32x4{0, 0, 0, 0};
       rb[u] = kin && t0 + row < a.rows ? *reinterpret_cast<const f32x4*>(B + (int64_t)row * a.d + k0 + lk) : f32x4{0, 0, 0, 0};
     }
   };
   load(0);
-  int buf = 0;
-  for (int k0 = 0; k0 < a.d; k0 += K, buf ^= 1) {
+  for (int k0 = 0; k0 < a.d; k0 += K) {
+    if (k0 > 0) __syncthreads();  // every wave is done with the step before
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      *reinterpret_cast<f32x4*>(&lds[buf][0][(lr + 32 * u) * P + lk]) = ra[u];
-      *reinterpret_cast<f32x4*>(&lds[buf][1][(lr + 32 * u) * P + lk]) = rb[u];
+    for (int u = 0; u < 4; ++u) {
+      *reinterpret_cast<f32x4*>(&lds[0][(lr + 16 * u) * P + lk]) = ra[u];
+      *reinterpret_cast<f32x4*>(&lds[1][(lr + 16 * u) * P + lk]) = rb[u];
     }
-    // this step's tiles are stored; the other buffer's readers passed the barrier before it is stored again
     __syncthreads();
     if (k0 + K < a.d) load(k0 + K);
-    const float* As = &lds[buf][0][(wm * 32 + l32) * P + 4 * hi];
-    const float* Bs = &lds[buf][1][(wn * 32 + l32) * P + 4 * hi];
+    const float* As = &lds[0][(wm * 32 + l32) * P + 4 * hi];
+    const float* Bs = &lds[1][(wn * 32 + l32) * P + 4 * hi];
 #pragma unroll
     for (int j = 0; j < K / 8; ++j) {
       const f32x4 x = *reinterpret_cast<const f32x4*>(As + 8 * j), y = *reinterpret_cast<const f32x4*>(Bs + 8 * j);
@@ -360,38 +360,40 @@ __global__ __launch_bounds__(256) void lp_rows_kernel(LpArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const float* z = a.logits + (int64_t)row * a.ldz;
   const int v0 = split * (256 * E);
+  const int y = a.labels[a.row0 + row];
+  const float zy = y >= v0 && y < min(a.V, v0 + 256 * E) ? z[y] : __uint_as_float(0x7FC00000u);
   float x[E];  // entry i: v0 + (i / 4 * 256 + tid) * 4 + i % 4; past the row -inf
   float m = -INFINITY;
 #pragma unroll
   for (int i = 0; i < E; i += 4) {
     const int v = v0 + (i / 4 * 256 + tid) * 4;
-    f32x4 y = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-    if (v < a.V) y = *reinterpret_cast<const f32x4*>(z + v);
+    f32x4 four = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    if (v < a.V) four = *reinterpret_cast<const f32x4*>(z + v);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      x[i + e] = v + e < a.V ? y[e] : -INFINITY;
+      x[i + e] = v + e < a.V ? four[e] : -INFINITY;
       m = fmaxf(m, x[i + e]);
     }
   }
+  m = wave_reduce(m, [](float x, float y) { return fmaxf(x, y); });
   float s = 0.0f, t = 0.0f;
-  const float m0 = m == -INFINITY ? 0.0f : m;
+  const float m0 = m == -INFINITY ? 0.0f : m, mb = m0 * kLog2e;
 #pragma unroll
   for (int i = 0; i < E; ++i) {
-    const float d = x[i] - m0, e = expf(d);
+    const float e = __builtin_amdgcn_exp2f(fmaf(x[i], kLog2e, -mb));
     s += e;
-    t += e == 0.0f ? 0.0f : d * e;
+    t = fmaf(fmaxf(x[i] - m0, -200.0f), e, t);  // e is 0 there: -inf times it would not be
   }
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) stats_join(m, s, t, __shfl_xor(m, o, 64), __shfl_xor(s, o, 64), __shfl_xor(t, o, 64));
+  auto add = [](float x, float y) { return x + y; };
+  s = wave_reduce(s, add);
+  t = wave_reduce(t, add);
   __shared__ float4 st[4];
   __shared__ Cand best[2][4];
   if (lane == 0) st[w] = make_float4(m, s, t, 0.0f);
   __syncthreads();
   if (tid == 0) {
     for (int i = 1; i < 4; ++i) stats_join(m, s, t, st[i].x, st[i].y, st[i].z);
-    const int y = a.labels[a.row0 + row];
-    a.stats[(int64_t)split * a.rows + row] =
-        make_float4(m, s, t, y >= v0 && y < min(a.V, v0 + 256 * E) ? z[y] : __uint_as_float(0x7FC00000u));
+    a.stats[(int64_t)split * a.rows + row] = make_float4(m, s, t, zy);
   }
   if (a.top == 0) return;
   // what is drawn, or past the row, becomes a NaN, which is better than nothing else
@@ -453,11 +455,16 @@ __global__ __launch_bounds__(256) void lp_join_kernel(LpArgs a) {
     stats_join(m, s, t, x.x, x.y, x.z);
     if (x.w == x.w) zy = x.w;
   }
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    stats_join(m, s, t, __shfl_xor(m, o, 64), __shfl_xor(s, o, 64), __shfl_xor(t, o, 64));
-    const float other = __shfl_xor(zy, o, 64);
-    if (other == other) zy = other;
+  {
+    auto add = [](float x, float y) { return x + y; };
+    const float mw = wave_reduce(m, [](float x, float y) { return fmaxf(x, y); });
+    // a lane without anything finite has (0, 0) here, or a NaN
+    const float d = m == -INFINITY ? 0.0f : m - mw, f = __builtin_amdgcn_exp2f(d * kLog2e);
+    t = wave_reduce(f * (t + d * s), add);
+    s = wave_reduce(f * s, add);
+    m = mw;
+    const uint64_t has = __ballot(zy == zy);  // one lane at most
+    zy = has ? __shfl(zy, __builtin_ctzll(has), 64) : zy;
   }
   if constexpr (T > 64) {
     if (lane == 0) parts[w] = make_float4(m, s, t, zy);
