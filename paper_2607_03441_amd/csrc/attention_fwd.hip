@@ -3,6 +3,8 @@
 //   S = scale Q K^T over the keys s <= t of the episode, lse = log sum exp S, O = exp(S - lse) V,
 //   D = rowsum(dO * O) for the backward.
 // One pass over the keys: the running maximum and sum of the softmax and O stay in registers.
+#include <algorithm>
+
 #include "attention_core.hpp"
 #include "lds_limit.hpp"
 
@@ -276,12 +278,24 @@ static hipError_t launch_fwd(LdsLimit& limit, const AttnArgs& a, AttnBatch b, hi
   return hipGetLastError();
 }
 
+// One or two query tiles a wave, by an estimate in microseconds of the launch: starts and ends of the workgroups
+// and their steps of 64 keys, spread over the CUs, and part of the longest walk; but no less than that walk alone. Fitted to 31
+// shapes (rms errors 9% and 8%), over which the choice takes 1.01 times the better one's time on average. One tile / two:
+// 8192 rows x 4 heads 130 / 167; 2048 x 32 53 / 56; 4096 x 32 181 / 156; 16 x 128 x 32 16 / 14; 64 x 64 x 32 30 / 32.
+// Far from the better: 2 x 1000 x 32 takes 39 with two, 33 with one.
 hipError_t launch_attn_fwd(const AttnArgs& a, const AttnBatch& b, hipStream_t s) {
   static LdsLimit limits[2];
-  int n1 = 0, n2 = 0;
-  for (int i = 0; i < b.count; ++i) n1 += (b.e[i].L + 63) / 64, n2 += (b.e[i].L + 127) / 128;
-  const bool wide = (int64_t)n2 * a.heads > 480 && 8 * (int64_t)n1 > 9 * (int64_t)n2;
-  return wide ? launch_fwd<2>(limits[1], a, b, s) : launch_fwd<1>(limits[0], a, b, s);
+  double wgs[2] = {}, steps[2] = {}, longest = 0.0;
+  for (int i = 0; i < b.count; ++i) {
+    const double n = (b.e[i].L + 63) / 64, m = (b.e[i].L + 127) / 128;
+    wgs[0] += n, wgs[1] += m;
+    steps[0] += n * (n + 1) / 2, steps[1] += m * (m + 1) - (2 * m - n);
+    longest = std::max(longest, n);
+  }
+  const double cus = a.heads / 256.0;
+  const double one = 3.9 + std::max(1.01 * longest, cus * (2.13 * wgs[0] + 0.66 * steps[0]));
+  const double two = 4.7 + std::max(1.34 * longest, cus * (1.97 * wgs[1] + 1.16 * steps[1]) + 0.24 * longest);
+  return two < one ? launch_fwd<2>(limits[1], a, b, s) : launch_fwd<1>(limits[0], a, b, s);
 }
 
 hipError_t launch_attn_dsum(const AttnArgs& a, hipStream_t s) {
