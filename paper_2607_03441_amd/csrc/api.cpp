@@ -526,14 +526,17 @@ attt_status attn_run(const void* q, const void* k, const void* v, const void* o,
   if (N == 0) return ATTT_OK;
   st = attn_pointers({q, k, v, o ? o : q, dout, dq, dk, dv, lse, dsum});
   if (st) return st;
-  std::vector<AttnSplit> splits;
+  AttnSplit first_splits[8];  // of the first launches; those of later ones are found twice
+  auto split_of = [&](int32_t e0) {
+    return attn_split(off + e0, std::min<int32_t>(kEpBatch, num_episodes - e0), heads, kv_heads, split);
+  };
   for (int32_t e0 = 0; e0 < num_episodes; e0 += kEpBatch) {
-    const AttnSplit sp = attn_split(off + e0, std::min<int32_t>(kEpBatch, num_episodes - e0), heads, kv_heads, split);
+    const AttnSplit sp = split_of(e0);
     if (workspace_bytes < sp.bytes)
       return fail(ATTT_ENOSPACE, "attention: workspace %zu bytes, need %zu", workspace_bytes, sp.bytes);
     if (sp.bytes && !workspace) return fail(ATTT_EINVAL, "attention: workspace is null");
     if (sp.bytes && !aligned256(workspace)) return fail(ATTT_EINVAL, "attention: workspace must be 256-byte aligned");
-    splits.push_back(sp);
+    if (e0 / kEpBatch < 8) first_splits[e0 / kEpBatch] = sp;
   }
   AttnArgs a{};
   a.q = static_cast<const bf16_t*>(q);
@@ -563,9 +566,10 @@ attt_status attn_run(const void* q, const void* k, const void* v, const void* o,
       for (int i = 0; i < head.count; ++i) head.e[i].L = std::min(head.e[i].L, kAttnExactRows);
       HIP_TRY(launch_attn(0, first, head, s), "attn_fwd_stats");
     }
-    b.tiles = splits[e0 / kEpBatch].tiles;
-    b.splits = splits[e0 / kEpBatch].splits;
-    b.chunk = splits[e0 / kEpBatch].chunk;
+    const AttnSplit sp = e0 / kEpBatch < 8 ? first_splits[e0 / kEpBatch] : split_of(e0);
+    b.tiles = sp.tiles;
+    b.splits = sp.splits;
+    b.chunk = sp.chunk;
     b.part = static_cast<float*>(workspace);
     for (int kernel = o ? 1 : 0; kernel < 3; ++kernel)
       HIP_TRY(launch_attn(kernel, a, b, s), kernel == 0 ? "attn_fwd_stats" : kernel == 1 ? "attn_dkdv" : "attn_dq");

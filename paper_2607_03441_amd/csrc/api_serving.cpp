@@ -206,7 +206,7 @@ extern "C" attt_status attt_kv4_attention(const void* q, const void* cache, int6
   a.lengths = lengths;
   a.o = static_cast<bf16_t*>(o);
   a.lse = lse;
-  a.max_length = max_length;
+  a.max_length = pages > 0 ? max_length : 0;  // no page, no sequence with a token
   a.N = N;
   a.heads = heads;
   a.kv_heads = kv_heads;
@@ -260,10 +260,10 @@ LpPlan lp_plan(int64_t N, int64_t V, int32_t dtype, int32_t top) {
   if (P.fused) {
     P.rows = std::min(N, kLpFusedRows);
     // Row tiles x splits workgroups, one per CU at a time: the splits with the fewest tiles one after the other, a
-    // workgroup's start and end counted as a third of a tile.
+    // workgroup's start and end counted as a third of a tile. (4096 workgroups bound the lists: 96 MiB.)
     const int64_t tiles_t = ceil_div(P.rows, 256), tiles_v = ceil_div(V, 256);
     double best = 0.0;
-    for (int64_t s = 1; s <= std::min<int64_t>(tiles_v, 256); ++s) {
+    for (int64_t s = 1; s <= std::min<int64_t>(tiles_v, 256) && (s == 1 || tiles_t * s <= 4096); ++s) {
       const double cost = (double)ceil_div(tiles_t * s, 256) * ((double)ceil_div(tiles_v, s) + 0.3);
       if (s == 1 || cost < best) best = cost, P.splits = (int32_t)s;
     }

@@ -96,7 +96,7 @@ def run(attt, s, **kw):
 CASES = [  # lengths, rows, heads, kv heads
     ([1], [1], 1, 1), ([128], [1], 4, 2), ([129], [1], 8, 1), ([2, 0, 300, 127], [1, 1, 1, 1], 4, 2),
     ([5], [5], 2, 2), ([131, 3], [7, 3], 6, 2), ([400, 17, 0, 256], [130, 17, 2, 128], 4, 2),
-    ([300], [300], 3, 1), ([1000, 2], [9, 5], 16, 2), ([700], [33], 8, 8), ([513], [40], 5, 1), ([90], [2], 56, 8)]
+    ([300], [300], 3, 1), ([5, 40, 3], [9, 64, 1], 4, 2), ([3, 0], [20, 20], 4, 4), ([1000, 2], [9, 5], 16, 2), ([700], [33], 8, 8), ([513], [40], 5, 1), ([90], [2], 56, 8)]
 
 
 @pytest.mark.parametrize("lengths,rows,H,kv", CASES)
@@ -208,6 +208,23 @@ def test_long_sequences_split(attt, rows, H, kv):
     assert np.array_equal(o, o2) and np.array_equal(lse, l2)  # bitwise repeatable
 
 
+def test_no_pages(attt):
+    """A cache without a page: only sequences without a token have a result. The calls with any are refused or NaN."""
+    import ctypes
+
+    import torch
+    q = torch.ones(2, 2, DH, dtype=torch.bfloat16, device="cuda")
+    o, lse = torch.zeros_like(q), torch.zeros(2, 2, device="cuda")
+    table = torch.zeros(2, 1, dtype=torch.int32, device="cuda")
+    length = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    L = attt.load()
+    attt._check(L.attt_kv4_attention(q.data_ptr(), q.data_ptr(), 0, table.data_ptr(), 1, length.data_ptr(), None, 2, 2, 2, 1, DH, 128,
+                                     ctypes.c_float(0.1), o.data_ptr(), lse.data_ptr(), None, 0, attt._stream_ptr()))
+    assert not o[0].any() and (lse[:, 0] == -np.inf).all() and torch.isnan(o[1]).all() and torch.isnan(lse[:, 1]).all()
+    with pytest.raises(attt.AtttError):
+        attt.kv4_attention(q, torch.empty(0, 1, okv.RECORD, dtype=torch.uint8, device="cuda"), table, length)
+
+
 def test_more_sequences_than_a_launch(attt):
     lengths = [(37 * e) % 200 for e in range(131)]
     s = make(lengths, [1] * 131, 2, 1, 61)
@@ -272,6 +289,18 @@ def test_captured_steps_follow_lengths(attt):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(d["cache"], other) and out[0].equal(want[0]) and out[1].equal(want[1]), n
+
+
+def test_many_equal_sequences(attt):
+    """Decoding batches around a launch's 64 sequences, and chunks of equal rows: the sequence is found by division."""
+    for E, rows, H, kv in ((1, 1, 8, 8), (63, 1, 4, 2), (64, 1, 2, 2), (65, 2, 4, 1), (5, 20, 4, 2), (3, 33, 4, 2)):
+        lengths = [rows + (53 * e) % 300 for e in range(E)]
+        s = make(lengths, [rows] * E, H, kv, 500 + E)
+        note(f"kv4: {E} sequences of {rows} rows each, {H} heads over {kv}")
+        cache, kh, vh, o, lse = run(attt, s, max_length=max(lengths))
+        want, wk, wv = expected(s)
+        assert np.array_equal(cache, want) and np.array_equal(kh, wk) and np.array_equal(vh, wv)
+        check_attention(s, want, o, lse)
 
 
 def test_other_stream(attt):

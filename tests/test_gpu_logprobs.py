@@ -55,7 +55,7 @@ def compare(got, r, d, exact, top):
 
 
 CASES = [(1, 8, 1, 1), (1, 64, 5, 5), (3, 72, 300, 7), (17, 128, 4096, 8), (33, 256, 4097, 20), (64, 64, 1000, 32),
-         (129, 136, 2051, 1), (300, 64, 513, 3), (513, 256, 8192, 0), (40, 512, 20001, 8), (700, 128, 3001, 20)]
+         (129, 136, 2051, 1), (300, 64, 513, 3), (513, 256, 8192, 0), (40, 512, 20001, 8), (700, 128, 3001, 20), (300, 64, 40001, 10), (520, 72, 30000, 3), (129, 64, 90001, 0), (260, 64, 39000, 11)]
 
 
 @pytest.mark.parametrize("bf16", [True, False])
@@ -80,7 +80,7 @@ def test_general_values(attt, bf16):
     compare(attt.token_logprobs(*dev(h, W, y, bf16), top=8), olp.token_logprobs(h, W, y, 8), 320, False, 8)
 
 
-@pytest.mark.parametrize("N", [5, 200])
+@pytest.mark.parametrize("N", [5, 200, 1200])
 @pytest.mark.parametrize("bf16", [True, False])
 def test_ties_take_the_lowest_ids(attt, N, bf16):
     """Many equal logits: blocks of equal head rows far apart, and rows that are all zero."""
@@ -90,9 +90,11 @@ def test_ties_take_the_lowest_ids(attt, N, bf16):
     r = olp.token_logprobs(h, W, y, 20)
     assert (r["ids"][1] == np.arange(20)).all()
     compare(attt.token_logprobs(*dev(h, W, y, bf16), top=20), r, 64, True, 20)
+    r["ids"], r["top"] = r["ids"][:, :9], r["top"][:, :9]
+    compare(attt.token_logprobs(*dev(h, W, y, bf16), top=9), r, 64, True, 9)
 
 
-@pytest.mark.parametrize("N", [7, 150])
+@pytest.mark.parametrize("N", [7, 150, 1700])
 @pytest.mark.parametrize("bf16", [True, False])
 def test_sorted_heads(attt, N, bf16):
     """Logits that grow, and that fall, along the vocabulary: every tile replaces the alternatives, or none does."""
@@ -106,10 +108,13 @@ def test_sorted_heads(attt, N, bf16):
     if bf16:  # 8 bits hold the first 188 steps
         W[:, 0] = np.minimum(W[:, 0], 187 / 512.0)
     y = np.arange(N).astype(np.int32)
-    compare(attt.token_logprobs(*dev(h, W, y, bf16), top=16), olp.token_logprobs(h, W, y, 16), d, True, 16)
+    r = olp.token_logprobs(h, W, y, 16)
+    compare(attt.token_logprobs(*dev(h, W, y, bf16), top=16), r, d, True, 16)
+    r["ids"], r["top"] = r["ids"][:, :10], r["top"][:, :10]
+    compare(attt.token_logprobs(*dev(h, W, y, bf16), top=10), r, d, True, 10)
 
 
-@pytest.mark.parametrize("N", [6, 140])
+@pytest.mark.parametrize("N", [6, 140, 13000])
 @pytest.mark.parametrize("bf16", [True, False])
 def test_labels_and_values_out_of_range(attt, N, bf16):
     """Labels outside the vocabulary; NaN and infinities in hidden states, alone in their rows' results."""

@@ -152,6 +152,9 @@ def test_logprob_refusals(L):
         attt.logprobs_workspace_size(4, 64, 100, attt.BF16, 33)
     # the rows staged at a time are bounded, however many there are
     assert attt.logprobs_workspace_size(1 << 20, 4096, 128256, attt.F32, 8) < 1 << 30
+    for N in (1, 128, 129, 300, 5000, 33024, 65536, 70000, 1 << 24):
+        for top in (0, 10, 32):
+            assert attt.logprobs_workspace_size(N, 4096, 128256, attt.BF16, top) < 1 << 29
 
 
 X = torch.zeros(4, 2, 128, dtype=torch.bfloat16)
