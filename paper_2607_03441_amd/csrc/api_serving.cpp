@@ -237,6 +237,7 @@ struct LpPlan {
   int64_t ldz = 0, rows = 0;   // staged logits: row length; rows at a time
   int32_t splits = 0, block = 0, chunk = 0;
   size_t off_stats = 0, off_lists = 0, total = 0;
+  bool joined() const { return fused || splits > 1; }  // rows of one staged chunk are finished at once
 };
 
 attt_status lp_check(int64_t N, int64_t d, int64_t V, int32_t dtype, int32_t top) {
@@ -281,8 +282,8 @@ LpPlan lp_plan(int64_t N, int64_t V, int32_t dtype, int32_t top) {
     P.block = (int32_t)P.rows;
   }
   P.off_stats = align256((size_t)P.rows * P.ldz * 4);
-  P.off_lists = P.off_stats + align256((size_t)P.rows * P.splits * sizeof(float4));
-  P.total = P.off_lists + (top > 0 ? align256((size_t)round_up(P.rows, P.block) * P.splits * top * sizeof(float2)) : 0);
+  P.off_lists = P.off_stats + (P.joined() ? align256((size_t)P.rows * P.splits * sizeof(float4)) : 0);
+  P.total = P.off_lists + (top > 0 && P.joined() ? align256((size_t)round_up(P.rows, P.block) * P.splits * top * sizeof(float2)) : 0);
   return P;
 }
 
@@ -340,7 +341,7 @@ extern "C" attt_status attt_token_logprobs(const void* hidden, const void* lm_he
       HIP_TRY(launch_lp_logits(dtype, a, s), "logprob_logits");
       HIP_TRY(launch_lp_rows(a, s), "logprob_rows");
     }
-    HIP_TRY(launch_lp_join(a, s), "logprob_join");
+    if (P.joined()) HIP_TRY(launch_lp_join(a, s), "logprob_join");
   }
   return ATTT_OK;
 }

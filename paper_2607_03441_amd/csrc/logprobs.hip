@@ -350,9 +350,26 @@ __global__ __launch_bounds__(512) void lp_fused_kernel(LpArgs a, int tiles_t, in
   }
 }
 
-// Statistics and the best `top` of 256 E logits of one staged row, E a thread, in registers. The best are drawn one
-// after the other: the best of each thread's, of each wave's, of the workgroup's; a thread keeps the best of
-// every 16, so that a draw costs its owner one scan of 16.
+// What a row's statistics and the label's logit say; the row's lse.
+__device__ __forceinline__ float write_row(const LpArgs& a, int64_t out, float m, float s, float t, float zy) {
+  const float ls = logf(s), lse = m + ls;
+  a.logp[out] = zy - lse;
+  if (a.entropy) a.entropy[out] = ls - t / s;
+  return lse;
+}
+// Alternative k of a row; a row that has no finite lse has none.
+__device__ __forceinline__ void write_top(const LpArgs& a, int64_t out, int k, Cand c, float lse) {
+  const bool ok = __builtin_isfinite(lse) && c.id != kNone;
+  a.top_ids[out * a.top + k] = ok ? (int32_t)c.id : -1;
+  a.top_logp[out * a.top + k] = ok ? c.z - lse : __uint_as_float(0x7FC00000u);
+}
+
+// Statistics and the best `top` of 256 E logits of one staged row, E a thread, in registers; where that is all of the row,
+// the results (a joining launch as well took 4.5 us more of 30 for 512 rows of 4096). The best are drawn one after the
+// other: the best of each thread's, of each wave's, of the workgroup's; a thread keeps the best of every 16, so that a
+// draw costs its owner one scan of 16. Bound by the draws, 0.7 us each where one row is on its way, not by the
+// reads. (Waves that draw for themselves, without a barrier, and a join of their lists: 20 alternatives of
+// 4096 x 5000 logits 268 us, this 212.)
 template <int E>
 __global__ __launch_bounds__(256) void lp_rows_kernel(LpArgs a) {
   constexpr int G = E / 16;
@@ -387,13 +404,18 @@ __global__ __launch_bounds__(256) void lp_rows_kernel(LpArgs a) {
   auto add = [](float x, float y) { return x + y; };
   s = wave_reduce(s, add);
   t = wave_reduce(t, add);
+  const bool all = a.splits == 1;
   __shared__ float4 st[4];
   __shared__ Cand best[2][4];
   if (lane == 0) st[w] = make_float4(m, s, t, 0.0f);
   __syncthreads();
+  float lse = 0.0f;  // thread 0's
   if (tid == 0) {
     for (int i = 1; i < 4; ++i) stats_join(m, s, t, st[i].x, st[i].y, st[i].z);
-    a.stats[(int64_t)split * a.rows + row] = make_float4(m, s, t, zy);
+    if (all)
+      lse = write_row(a, a.row0 + row, m, s, t, zy);
+    else
+      a.stats[(int64_t)split * a.rows + row] = make_float4(m, s, t, zy);
   }
   if (a.top == 0) return;
   // what is drawn, or past the row, becomes a NaN, which is better than nothing else
@@ -425,7 +447,12 @@ __global__ __launch_bounds__(256) void lp_rows_kernel(LpArgs a) {
 #pragma unroll
     for (int i = 1; i < 4; ++i)
       if (better(best[n & 1][i], b)) b = best[n & 1][i];
-    if (tid == 0) a.lists[lp_list(a, row, split, n)] = make_float2(b.z, __uint_as_float(b.id));
+    if (tid == 0) {
+      if (all)
+        write_top(a, a.row0 + row, n, b, lse);
+      else
+        a.lists[lp_list(a, row, split, n)] = make_float2(b.z, __uint_as_float(b.id));
+    }
     if (b.id != kNone && b.id == c.id) {
       c = {-INFINITY, kNone};
 #pragma unroll
@@ -475,11 +502,7 @@ __global__ __launch_bounds__(256) void lp_join_kernel(LpArgs a) {
       if (parts[i].w == parts[i].w) zy = parts[i].w;
     }
   }
-  const float ls = logf(s), lse = m + ls;
-  if (id == 0) {
-    a.logp[out] = zy - lse;
-    if (a.entropy) a.entropy[out] = ls - t / s;
-  }
+  const float lse = id == 0 ? write_row(a, out, m, s, t, zy) : 0.0f;
   auto entry = [&](int list, int k) -> Cand {
     if (list >= a.splits || k >= a.top) return {-INFINITY, kNone};
     const float2 x = a.lists[lp_list(a, row, list, k)];
@@ -516,11 +539,7 @@ __global__ __launch_bounds__(256) void lp_join_kernel(LpArgs a) {
         search(false, c);
       }
     }
-    if (id == 0) {
-      const bool ok = __builtin_isfinite(lse) && c.id != kNone;  // a row that has no finite lse has no alternatives
-      a.top_ids[out * a.top + k] = ok ? (int32_t)c.id : -1;
-      a.top_logp[out * a.top + k] = ok ? c.z - lse : __uint_as_float(0x7FC00000u);
-    }
+    if (id == 0) write_top(a, out, k, c, lse);
   }
 }
 
