@@ -4,6 +4,7 @@
 //   D = rowsum(dO * O) for the backward.
 // One pass over the keys: the running maximum and sum of the softmax and O stay in registers.
 #include <algorithm>
+#include <cmath>
 
 #include "attention_core.hpp"
 #include "lds_limit.hpp"
@@ -41,14 +42,20 @@ __device__ __forceinline__ bf16x8 swizzled_trfrag(const uint8_t* R, int j, int u
 // O and lse of one (query head, 64 QT-query block). Wave w owns queries 16 QT w .. + 16 QT - 1 as QT tiles of
 // 16, their Q fragments in registers as the B operand of S^T = K Q^T, so that each lane holds 16 scores of
 // its own query of a tile. exp(S - m), rounded to bf16 once (it is a weight in [0, 2^8]; the
-// rounding's 2^-9 is that of O itself), is then directly the B operand of O^T = V^T P^T: the contraction
+// rounding's 2^-8 at most is that of O itself), is then directly the B operand of O^T = V^T P^T: the contraction
 // runs over the keys in the order the lane holds them, and V^T comes from the row-major V tile through
 // transposing reads in that order. A lane's O values are all of its own query, so the factor by which an
 // older maximum is replaced is one register per tile. It is applied only where a maximum has grown by more than
 // 2^8: until then the weights stay below 2^8, which costs no precision in float32 or bf16.
-template <int QT>
-__global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a, AttnBatch b) {
-  constexpr int QBLK = 64 * QT;
+// Bound by the chain product -> maximum -> exp2 -> product of a block of keys, with two waves a SIMD to fill its
+// gaps: 8192 rows, 32 heads over 8, in 525 us, 1.05 PFLOP/s of the causal half. (K and V through registers into padded rows
+// 1333 us; fragments read one block ahead and maxima by swaps 567 -> 535; three blocks in flight in four buffers, one
+// workgroup a CU, slower at every length; a raised wave priority around the products 580.)
+// With WALKS = 2 a second set of four waves takes the odd blocks of keys of the same queries, and the two sums are joined
+// at the end through LDS: half as long a chain.
+template <int QT, int WALKS>
+__global__ __launch_bounds__(256 * WALKS, 2 / WALKS) void attn_fwd_kernel(AttnArgs a, AttnBatch b) {
+  constexpr int QBLK = 64 * QT, kBufs = 2 * WALKS - 1;  // block kb lies in buffer kb & kBufs
   int ei, slot, qb;
   attn_locate(b, a.heads, true, ei, slot, qb);
   const AttnEp E = b.e[ei];
@@ -57,8 +64,9 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a, AttnBatch 
   const int h = a.heads % 8 == 0 ? slot % 8 * (a.heads / 8) + slot / 8 : slot;
   const int kh = h / (a.heads / a.kv_heads);
   const int q0 = qb * QBLK, nq = min(QBLK, E.L - q0);
-  extern __shared__ __align__(16) uint8_t smem[];  // two buffers of [K tile][V tile], then found[2]
-  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  extern __shared__ __align__(16) uint8_t smem[];  // two buffers of [K tile][V tile] a walk, then found[]
+  const int tid = threadIdx.x & 255, walk = WALKS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0;
+  const int lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, q4 = lane >> 4;
   const int64_t qs = (int64_t)a.heads * DH, ks = (int64_t)a.kv_heads * DH;
   bf16x8 qf[QT][4];
@@ -87,7 +95,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a, AttnBatch 
     const int64_t at = ((int64_t)(E.row0 + k0) * a.kv_heads + kh) * DH;
     const int bytes = (int)(((int64_t)(nk - 1) * ks + DH) * 2);
     const __amdgpu_buffer_rsrc_t rk = buffer_rsrc(a.k + at, bytes), rv = buffer_rsrc(a.v + at, bytes);
-    uint8_t* dst = smem + (kb & 1) * kFwdBuf + w * 1024;
+    uint8_t* dst = smem + (kb & kBufs) * kFwdBuf + w * 1024;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (__attribute__((address_space(3))) void*)(dst + i * 4096), 16,
@@ -98,33 +106,33 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a, AttnBatch 
   };
   // Where some queries do not see all keys of a block, a weight of 0 does not hide an infinity or a NaN in V from the
   // product. Such entries are taken out of the tile, and the block's number in found[] says that there were some.
-  int* found = reinterpret_cast<int*>(smem + 2 * kFwdBuf);
-  if (tid < 2) found[tid] = -1;
-  load(0);
-  for (int kb = 0; kb <= kb_last; ++kb) {
-    const int k0 = kb * BLK;
+  int* found = reinterpret_cast<int*>(smem + 2 * WALKS * kFwdBuf);
+  if (threadIdx.x < 2 * WALKS) found[threadIdx.x] = -1;
+  if (walk <= kb_last) load(walk);
+  for (int step = 0; step <= kb_last; step += WALKS) {
+    const int kb = step + walk, k0 = kb * BLK;
     // This wave's loads have landed; then every wave's have, and every wave is done with the other buffer.
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
-    if (kb < kb_last) load(kb + 1);  // the next key block loads while this one computes
-    uint8_t* Ks = smem + (kb & 1) * kFwdBuf;
+    if (kb + WALKS <= kb_last) load(kb + WALKS);  // the next key block loads while this one computes
+    uint8_t* Ks = smem + (kb & kBufs) * kFwdBuf;
     uint8_t* Vs = Ks + kFwdTile;
-    if (kb >= kb_mask) {
+    if (step + WALKS > kb_mask) {
       int id = tid;
       asm volatile("" : "+v"(id));  // its addresses are not kept across the loop
 #pragma unroll 1
-      for (int i = 0; i < 4; ++i) {
+      for (int i = kb >= kb_mask && kb <= kb_last ? 0 : 4; i < 4; ++i) {
         u32x4* piece = reinterpret_cast<u32x4*>(Vs + (id + 256 * i) * 16);
         u32x4 x = *piece;
         if (take_nonfinite(x)) {
           *piece = x;
-          found[kb & 1] = kb;
+          found[kb & kBufs] = kb;
         }
       }
       __syncthreads();
     }
-    // A wave whose queries all precede the block has nothing to add.
-    if (k0 <= wq0 + 16 * QT - 1) {
+    // A wave whose queries all precede the block has nothing to add; nor is there any past the last.
+    if (kb <= kb_last && k0 <= wq0 + 16 * QT - 1) {
       f32x4 st[QT][4];  // S^T[16 tt + 4 q4 + r][query]
 #pragma unroll
       for (int c = 0; c < QT; ++c)
@@ -208,7 +216,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a, AttnBatch 
         __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
         __builtin_amdgcn_sched_group_barrier(0x008, QT, 0);
       }
-      if (kb >= kb_mask && found[kb & 1] == kb) {  // the entries taken out, for the queries that see them
+      if (kb >= kb_mask && found[kb & kBufs] == kb) {  // the entries taken out, for the queries that see them
         int id = lane;
         asm volatile("" : "+v"(id));
         const bf16_t* vb = a.v + ((int64_t)(E.row0 + k0) * a.kv_heads + kh) * DH + 4 * (id >> 4);
@@ -230,10 +238,39 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a, AttnBatch 
       }
     }
   }
+  float lsum[QT];
+#pragma unroll
+  for (int c = 0; c < QT; ++c) lsum[c] = rows_sum(l[c]);
+  if constexpr (WALKS > 1) {
+    f32x4(*ex)[QT][8][64] = reinterpret_cast<f32x4(*)[QT][8][64]>(smem);
+    float2(*ml)[QT][64] = reinterpret_cast<float2(*)[QT][64]>(smem + 4 * sizeof(*ex));
+    static_assert(4 * (sizeof(*ex) + sizeof(*ml)) <= 2 * WALKS * kFwdBuf, "LDS");
+    __syncthreads();
+    if (walk) {
+#pragma unroll
+      for (int c = 0; c < QT; ++c) {
+        ml[w][c][lane] = make_float2(m[c], lsum[c]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) ex[w][c][j][lane] = o[c][j];
+      }
+    }
+    __syncthreads();
+    if (walk) return;
+#pragma unroll
+    for (int c = 0; c < QT; ++c) {
+      const float2 other = ml[w][c][lane];
+      const float mn = fmaxf(m[c], other.x), ms = mn == -INFINITY ? 0.0f : mn;
+      const float fa = __builtin_amdgcn_exp2f(m[c] - ms), fb = __builtin_amdgcn_exp2f(other.x - ms);
+      m[c] = mn;
+      lsum[c] = lsum[c] * fa + other.y * fb;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o[c][j] = o[c][j] * fa + ex[w][c][j][lane] * fb;
+    }
+  }
 #pragma unroll
   for (int c = 0; c < QT; ++c) {
     const int qry = 16 * QT * w + 16 * c + l16;
-    const float lc = rows_sum(l[c]);
+    const float lc = lsum[c];
     if (qry < nq) {
       if (q4 == 0) a.lse[(int64_t)h * a.N + E.row0 + q0 + qry] = m[c] / kLog2e + logf(lc);
       const float inv = 1.0f / lc;
@@ -262,10 +299,10 @@ __global__ __launch_bounds__(256) void attn_dsum_kernel(AttnArgs a) {
   if ((threadIdx.x & 15) == 0) a.dsum[(i % a.heads) * a.N + i / a.heads] = s;
 }
 
-template <int QT>
+template <int QT, int WALKS>
 static hipError_t launch_fwd(LdsLimit& limit, const AttnArgs& a, AttnBatch b, hipStream_t s) {
-  constexpr size_t lds = 2 * (size_t)kFwdBuf + 16;
-  if (hipError_t e = limit.raise((const void*)attn_fwd_kernel<QT>, lds)) return e;
+  constexpr size_t lds = 2 * WALKS * (size_t)kFwdBuf + 16;
+  if (hipError_t e = limit.raise((const void*)attn_fwd_kernel<QT, WALKS>, lds)) return e;
   int n = 0;
   for (int i = 0; i < b.count; ++i) {
     b.e[i].blocks = (b.e[i].L + 64 * QT - 1) / (64 * QT);
@@ -274,17 +311,19 @@ static hipError_t launch_fwd(LdsLimit& limit, const AttnArgs& a, AttnBatch b, hi
   }
   if (n <= 0) return hipSuccess;
   KernelTimer t(K_ATTN_PROMPT, s);
-  hipLaunchKernelGGL(attn_fwd_kernel<QT>, dim3(n), dim3(256), lds, s, a, b);
+  hipLaunchKernelGGL((attn_fwd_kernel<QT, WALKS>), dim3(n), dim3(256 * WALKS), lds, s, a, b);
   return hipGetLastError();
 }
 
-// One or two query tiles a wave, by an estimate in microseconds of the launch: starts and ends of the workgroups
-// and their steps of 64 keys, spread over the CUs, and part of the longest walk; but no less than that walk alone. Fitted to 31
-// shapes (rms errors 9% and 8%), over which the choice takes 1.01 times the better one's time on average. One tile / two:
-// 8192 rows x 4 heads 130 / 167; 2048 x 32 53 / 56; 4096 x 32 181 / 156; 16 x 128 x 32 16 / 14; 64 x 64 x 32 30 / 32.
-// Far from the better: 2 x 1000 x 32 takes 39 with two, 33 with one.
+// One or two query tiles a wave and one or two walks, by an estimate in microseconds of the launch: starts and ends of the
+// workgroups and their steps of 64 keys, spread over the CUs, against the longest walk; the larger of the two and a part of the
+// other. Fitted to 55 shapes of 64 to 30000 rows (rms errors 7 to 9%), over which the choice takes 1.014 times the
+// best one's time on average (without two walks 1.096). One tile / two / one and two walks / two and two walks:
+// 100 rows x 16 heads 5.9 / 7.8 / 6.2 / 8.8; 4096 x 4 63 / 86 / 46 / 68; 2048 x 16 38.5 / 48.5 / 33.1 / 40.4; 8192 x 8
+// 175 / 189 / 189 / 153; 8192 x 32 658 / 525 / 738 / 575; 16 x 128 x 32 15.9 / 14.3 / 25.2 / 20.9.
+// Farthest from the best: 2 x 1000 x 32 takes 40 with the chosen two tiles, 33 with one.
 hipError_t launch_attn_fwd(const AttnArgs& a, const AttnBatch& b, hipStream_t s) {
-  static LdsLimit limits[2];
+  static LdsLimit limits[4];
   double wgs[2] = {}, steps[2] = {}, longest = 0.0;
   for (int i = 0; i < b.count; ++i) {
     const double n = (b.e[i].L + 63) / 64, m = (b.e[i].L + 127) / 128;
@@ -292,10 +331,25 @@ hipError_t launch_attn_fwd(const AttnArgs& a, const AttnBatch& b, hipStream_t s)
     steps[0] += n * (n + 1) / 2, steps[1] += m * (m + 1) - (2 * m - n);
     longest = std::max(longest, n);
   }
+  struct Fit {
+    double start, chain, wg, step, rest;
+  };
+  static constexpr Fit fits[4] = {
+      {3.95, 0.93, 2.10, 0.59, 0.14}, {5.41, 1.16, 2.40, 0.95, 0.30}, {4.97, 1.35, 4.53, 0.65, 0.0}, {7.03, 1.93, 5.84, 1.01, 0.04}};
   const double cus = a.heads / 256.0;
-  const double one = 3.9 + std::max(1.01 * longest, cus * (2.13 * wgs[0] + 0.66 * steps[0]));
-  const double two = 4.7 + std::max(1.34 * longest, cus * (1.97 * wgs[1] + 1.16 * steps[1]) + 0.24 * longest);
-  return two < one ? launch_fwd<2>(limits[1], a, b, s) : launch_fwd<1>(limits[0], a, b, s);
+  int best = 0;
+  double least = 0.0;
+  for (int v = 0; v < 4; ++v) {
+    const Fit& f = fits[v];
+    const double chain = f.chain * (v < 2 ? longest : std::floor((longest + 1) / 2));
+    const double work = cus * (f.wg * wgs[v & 1] + f.step * steps[v & 1]);
+    const double time = f.start + std::max(chain, work) + f.rest * std::min(chain, work);
+    if (v == 0 || time < least) least = time, best = v;
+  }
+  return best == 0   ? launch_fwd<1, 1>(limits[0], a, b, s)
+         : best == 1 ? launch_fwd<2, 1>(limits[1], a, b, s)
+         : best == 2 ? launch_fwd<1, 2>(limits[2], a, b, s)
+                     : launch_fwd<2, 2>(limits[3], a, b, s);
 }
 
 hipError_t launch_attn_dsum(const AttnArgs& a, hipStream_t s) {

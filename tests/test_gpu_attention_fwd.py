@@ -108,6 +108,43 @@ def test_growing_scores(attt):
     check_forward(host(o), host(lse), host(q), host(k), host(v), np.array([0, N]))
 
 
+@pytest.mark.parametrize("H,kv,off", [(8, 2, [0, 700]), (2, 1, [0, 1, 900, 901, 1700]), (16, 8, [0, 3000]), (16, 4, [0, 2050])])
+def test_long_walks(attt, H, kv, off):
+    """Few long walks over the keys, which two sets of waves share: one query tile a wave, and two."""
+    off = np.array(off, np.int64)
+    note(f"attention_fwd: {H} heads over {kv}, episodes {np.diff(off).tolist()}")
+    q, k, v, _ = inputs(int(off[-1]), H, kv, 300 + H)
+    o, lse = attt.attention_fwd(dev_dense(q), dev_dense(k), dev_dense(v), row_offsets=off)
+    g = H // kv
+    for c in (0, kv - 1):  # the first and the last key/value head
+        h = slice(c * g, c * g + g)
+        check_forward(host(o)[:, h], host(lse)[h], q.f32[:, h], k.f32[:, c:c + 1], v.f32[:, c:c + 1], off)
+
+
+@pytest.mark.parametrize("H,kv,N,rows", [(4, 2, 700, (0, 70, 130, 699)), (16, 8, 3000, (5, 64, 2944, 2999))])
+def test_nonfinite_in_long_walks(attt, H, kv, N, rows):
+    import torch
+    q, k, v, _ = (dev_dense(x) for x in inputs(N, H, kv, 27))
+    o0, l0 = attt.attention_fwd(q, k, v)
+    g = H // kv
+    for at in rows:
+        for what in (float("nan"), float("inf")):
+            w = v.clone()
+            w[at, 0, 5] = what
+            o, lse = attt.attention_fwd(q, k, w)
+            note(f"{what} in v of row {at} of {N}")
+            assert torch.equal(o[:at], o0[:at]) and torch.equal(o[:, g:], o0[:, g:]) and torch.equal(lse, l0)
+            assert not torch.isfinite(o[at:, :g, 5]).any()
+            rest = [c for c in range(DH) if c != 5]
+            assert torch.equal(o[:, :, rest], o0[:, :, rest])
+        x = k.clone()
+        x[at, 0, 5] = float("nan")
+        o, lse = attt.attention_fwd(q, x, v)
+        note(f"nan in k of row {at} of {N}")
+        assert torch.equal(o[:at], o0[:at]) and torch.equal(lse[:, :at], l0[:, :at]) and torch.equal(o[:, g:], o0[:, g:])
+        assert torch.isnan(o[at:, :g]).all() and torch.isnan(lse[:g, at:]).all()
+
+
 def test_nonfinite_in_masked_places(attt):
     """A NaN or an infinity in a later token's key or value, or in another episode, changes no bit before it."""
     import torch
