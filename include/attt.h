@@ -14,6 +14,11 @@
  *   attt_weighted_ce_fwd_bwd  weighted CE through the frozen LM head, loss and dL/dh (Eq. 10)
  *   attt_lora_grad            LoRA dA / dB of the adapted projections (Sec. 3.1, Appendix C)
  *   attt_lora_sgd_step        the adapter step theta <- theta - lr grad (Eq. 2, Algorithm 1)
+ * and beside the step
+ *   attt_attention_fwd, attt_attention_bwd_saved
+ *                             the adapted attention block over whole prompts, and its backward from what was saved
+ *   attt_kv4_*                a paged key/value cache in 4 bits and the attention of new tokens over it
+ *   attt_token_logprobs       what the model says about given tokens: log-probabilities, entropies, alternatives
  *
  * Conventions shared by every call
  *   - Data pointers are device pointers unless a parameter says "host". The caller owns all
@@ -169,7 +174,7 @@ attt_status attt_attention_bwd_split(const void* q, const void* k, const void* v
  *   workspace  as for attt_attention_bwd_split (attt_attention_workspace_size bytes; NULL with 0
  *              bytes: one workgroup per key block, as attt_attention_bwd)
  * D is formed from the O given, that is from its bf16 values, but for the first 128 rows of every episode, where it is
- * computed as by attt_attention_bwd. */
+ * computed as by attt_attention_bwd. Outputs overlap neither inputs nor each other. */
 attt_status attt_attention_fwd(const void* q, const void* k, const void* v, const int64_t* row_offsets,
                                int32_t num_episodes, int64_t N, int32_t heads, int32_t kv_heads,
                                int32_t head_dim, float scale, void* o, float* lse, void* stream);
@@ -509,6 +514,7 @@ attt_status attt_lora_hot_swap(const attt_lora_swap_item* items, int32_t count, 
  * o, lse        device bf16 [N][heads][128], float32 [heads][N] (written)
  * workspace     attt_kv4_attention_workspace_size bytes for the same offsets, heads and max_length
  *               (may be 0), 256-byte aligned
+ * Outputs overlap neither inputs nor each other.
  * lengths and the table are read on the device, so a captured graph follows them. What the host
  * cannot see is reported in the outputs: rows of a sequence with a length above max_length (append: above 128
  * table_width), or whose table names a page outside [0, pages), are NaN (append: such rows are not
@@ -549,6 +555,7 @@ attt_status attt_kv4_attention(const void* q, const void* cache, int64_t pages, 
  * logp          device float [N];  entropy: device float [N] or NULL
  * top_ids, top_logp  device int32, float [N][top] (not read for top = 0)
  * workspace     attt_logprobs_workspace_size bytes, 256-byte aligned
+ * Outputs overlap neither inputs nor each other.
  * A label outside [0, V): logp is NaN, the rest as ever. A row without a finite lse (a NaN or +inf logit, or only
  * -inf): NaN everywhere, ids -1. Errors (before any HIP call): ATTT_EINVAL, ATTT_ENOSPACE, ATTT_EUNSUPPORTED.
  * ------------------------------------------------------------------------------------ */

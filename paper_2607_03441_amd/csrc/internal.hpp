@@ -197,6 +197,7 @@ hipError_t launch_attn_dsum(const AttnArgs& a, hipStream_t s);  // of all N rows
 // ---- serving: the 4-bit key/value cache ------------------------------------------------------------
 constexpr int kKv4Page = 128;      // tokens per page
 constexpr int kKv4Record = 17152;  // bytes of one (page, key/value head): 134 per token
+constexpr int kKv4ChunkRows = 128; // query rows of a workgroup where a head's group has many
 struct Kv4Args {
   const bf16_t* q;         // [N][heads][128]
   const bf16_t* k;         // append: [N][kv_heads][128]
@@ -213,7 +214,7 @@ struct Kv4Args {
   int64_t pages, width, max_length, N;
   int32_t heads, kv_heads;
   int32_t chunk, splits;   // pages per split, splits of the longest sequence
-  int32_t block_rows;      // query rows of a head's group per workgroup: 16, 64 or 128
+  int32_t block_rows;      // query rows of a head's group per workgroup: 16 or kKv4ChunkRows
   float scale;
 };
 struct Kv4Seq {

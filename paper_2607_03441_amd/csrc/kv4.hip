@@ -60,7 +60,8 @@ __device__ __forceinline__ bf16x8 widen(uint32_t x, float scale) {
 // token, eight elements each, two tokens after the other with both loads on their way: the maxima of its key blocks
 // (4 lanes) and of its value row (16 lanes) meet in shuffles. Key codes go to the page at once; value codes are
 // turned through LDS, and each piece is written by one thread, which keeps the codes of the tokens that were there.
-// (A workgroup per page, 16 tokens at a time, took 44 us for 16 x 512 rows of 8 heads.)
+// Bound by memory: 16 x 512 rows of 8 heads, 76 MB with what they stand for, in 18 us, 4.2 TB/s. (A workgroup per page, 16
+// tokens at a time, took 44 us.) One row of each of 16 sequences takes 5 us, the latency of length, page id and page.
 __global__ __launch_bounds__(256) void kv4_append_kernel(Kv4Args a, Kv4Batch b) {
   const Kv4Seq S = find_seq(b, blockIdx.x);
   const int local = (int)blockIdx.x - S.wg_begin;
@@ -223,9 +224,11 @@ struct Kv4Work {
     const int local = (int)blockIdx.x - S.wg_begin;
     kh = local % a.kv_heads;
     const int sb = local / a.kv_heads;
-    split = sb % a.splits;
-    rb = sb / a.splits;
     g = a.heads / a.kv_heads;
+    // a split's row blocks side by side: they read the same pages, through one XCD's L2 where kv_heads is a multiple of 8
+    const int blocks = (S.n * g + a.block_rows - 1) / a.block_rows;
+    rb = sb % blocks;
+    split = sb / blocks;
     int64_t len = a.lengths[S.seq];
     bad = len > a.max_length;
     if (len < 0 || bad) len = 0;
@@ -322,6 +325,9 @@ __device__ __forceinline__ void write_rows(const Kv4Args& a, const Kv4Work& k, i
 // the lane's registers and its three partner lanes. Weight times value scale is the B operand of O^T = V^T P^T. A
 // page's keys are asked for while the one before is multiplied with its values, and its values while
 // its keys are. At the end the waves' sums are joined in a fixed order through LDS.
+// Bound by the reads: one row of 8 episodes of 8192 to 131072 tokens (32 heads over 8) 632 MB in 117 us, 5.4 TB/s. At up to
+// 4000 tokens of 16 episodes 38 MB in 12.5 us: the latency of length, page id, page and product one after the other (page
+// ids and rows asked for before the length is known: the same).
 __global__ __launch_bounds__(256, 2) void kv4_decode_kernel(Kv4Args a, Kv4Batch b) {
   Kv4Work k;
   if (k.locate(a, b)) return;
@@ -413,10 +419,15 @@ __global__ __launch_bounds__(256, 2) void kv4_decode_kernel(Kv4Args a, Kv4Batch 
   if (w == 0) write_rows(a, k, l16, m, l, o, q4);
 }
 
-// Attention of 64 RT query rows per workgroup (prompts in chunks): every wave owns RT tiles of 16 rows and goes over all
+// Attention of 128 query rows per workgroup (prompts in chunks): every wave owns two tiles of 16 rows and goes over all
 // pages of the split, which lie in LDS as they are in the cache, the next one on its way. Nothing is joined between the waves.
-template <int RT>
+// Bound by issue: a page of 128 rows takes a wave 4 us, of which the products are a third; every wave widens all codes and
+// takes its exponentials, and two waves share a SIMD. 64 rows of 4 sequences of 512 to 8200 tokens (32 heads
+// over 8) in 39 us. With the join, when a split's row blocks were far apart: pages in each wave's registers instead of LDS
+// 80 us, this 56; two sets of four waves on alternate pages 61; one row tile a wave 57. Side by side: 50. Four row tiles a
+// wave, or fragments read a product ahead, spill.
 __global__ __launch_bounds__(256, 2) void kv4_chunk_kernel(Kv4Args a, Kv4Batch b) {
+  constexpr int RT = kKv4ChunkRows / 64;
   constexpr int PT = 4;  // tiles of 16 tokens whose scores are held at a time
   Kv4Work k;
   if (k.locate(a, b)) return;
@@ -510,7 +521,9 @@ __global__ __launch_bounds__(256, 2) void kv4_chunk_kernel(Kv4Args a, Kv4Batch b
     write_rows(a, k, 16 * RT * w + 16 * c + l16, m[c], bad ? __uint_as_float(0x7FC00000u) : rows_sum(l[c]), o[c], q4);
 }
 
-// Joins the splits of a row in their order. One wave per (row, query head), two elements a lane.
+// Joins the splits of a row in their order. One wave per (row, query head), two elements a lane, eight splits' loads on their
+// way. Bound by memory where there are many rows (64 x 4 rows x 32 heads, up to 13 splits: 28 MB in 8.6 us), by latency
+// otherwise (16 rows: 3.3 us).
 __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Args a, Kv4Batch b, int64_t rows) {
   const int lane = threadIdx.x & 63, R = a.block_rows;
   const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);  // (row of the batch, head)
@@ -595,10 +608,9 @@ static hipError_t launch_blocks(K kernel, LdsLimit& limit, size_t lds, const Kv4
 }
 
 hipError_t launch_kv4_attention(const Kv4Args& a, const Kv4Batch& b, hipStream_t s) {
-  static LdsLimit limits[3];
-  return a.block_rows == 16   ? launch_blocks(kv4_decode_kernel, limits[0], 0, a, b, s)
-         : a.block_rows == 64 ? launch_blocks(kv4_chunk_kernel<1>, limits[1], 2 * kChunkBuf, a, b, s)
-                              : launch_blocks(kv4_chunk_kernel<2>, limits[2], 2 * kChunkBuf, a, b, s);
+  static LdsLimit limits[2];
+  return a.block_rows == 16 ? launch_blocks(kv4_decode_kernel, limits[0], 0, a, b, s)
+                            : launch_blocks(kv4_chunk_kernel, limits[1], 2 * kChunkBuf, a, b, s);
 }
 
 }  // namespace attt

@@ -208,6 +208,18 @@ def test_long_sequences_split(attt, rows, H, kv):
     assert np.array_equal(o, o2) and np.array_equal(lse, l2)  # bitwise repeatable
 
 
+@pytest.mark.parametrize("lengths,rows,H,kv", [([2500, 0, 64, 1333, 640, 70], [64] * 6, 4, 1), ([700, 130, 125], [125] * 3, 4, 2),
+                                               ([1500, 1, 0, 900, 1400], [1, 1, 1, 100, 1], 8, 2), ([2000, 90], [9, 9], 10, 1)])
+def test_row_blocks_beside_each_other(attt, lengths, rows, H, kv):
+    """Many query rows of a head's group: whole chunks, chunks beside single tokens, and few rows past a block."""
+    s = make(lengths, rows, H, kv, 70 + sum(rows))
+    note(f"kv4 row blocks: lengths {lengths}, new rows {rows}, {H} heads over {kv}")
+    cache, _, _, o, lse = run(attt, s, max_length=max(lengths))
+    want, _, _ = expected(s)
+    assert np.array_equal(cache, want)
+    check_attention(s, want, o, lse)
+
+
 def test_no_pages(attt):
     """A cache without a page: only sequences without a token have a result. The calls with any are refused or NaN."""
     import ctypes
