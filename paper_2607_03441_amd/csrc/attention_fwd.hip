@@ -47,10 +47,11 @@ __device__ __forceinline__ bf16x8 swizzled_trfrag(const uint8_t* R, int j, int u
 // transposing reads in that order. A lane's O values are all of its own query, so the factor by which an
 // older maximum is replaced is one register per tile. It is applied only where a maximum has grown by more than
 // 2^8: until then the weights stay below 2^8, which costs no precision in float32 or bf16.
-// Bound by the chain product -> maximum -> exp2 -> product of a block of keys, with two waves a SIMD to fill its
-// gaps: 8192 rows, 32 heads over 8, in 525 us, 1.05 PFLOP/s of the causal half. (K and V through registers into padded rows
-// 1333 us; fragments read one block ahead and maxima by swaps 567 -> 535; three blocks in flight in four buffers, one
-// workgroup a CU, slower at every length; a raised wave priority around the products 580.)
+// 8192 rows, 32 heads over 8: 506 us, 1.09 PFLOP/s of the causal half. The matrix cores and the vector ALU are each busy
+// about half the time; that the two waves of a SIMD take turns at them is not to be had by priorities (of the products,
+// 580 us, or of one of the waves: no change) nor by products under the other half's exponentials in one wave (the same).
+// K and V through registers into padded rows took 1333 us; three blocks in flight in four buffers, one workgroup a CU, were
+// slower at every length.
 // With WALKS = 2 a second set of four waves takes the odd blocks of keys of the same queries, and the two sums are joined
 // at the end through LDS: half as long a chain.
 template <int QT, int WALKS>
@@ -109,7 +110,10 @@ __global__ __launch_bounds__(256 * WALKS, 2 / WALKS) void attn_fwd_kernel(AttnAr
   int* found = reinterpret_cast<int*>(smem + 2 * WALKS * kFwdBuf);
   if (threadIdx.x < 2 * WALKS) found[threadIdx.x] = -1;
   if (walk <= kb_last) load(walk);
-  for (int step = 0; step <= kb_last; step += WALKS) {
+  // A step of each walk. TAIL: some query does not see all keys. The two kinds are loops of their own: masks behind a branch
+  // in one loop made the compiler copy all of O in every step, where a maximum's replacement joins (534 us instead of 506).
+  auto walk_step = [&](int step, auto tail) {
+    constexpr bool TAIL = decltype(tail)::value;
     const int kb = step + walk, k0 = kb * BLK;
     // This wave's loads have landed; then every wave's have, and every wave is done with the other buffer.
     __builtin_amdgcn_s_waitcnt(0);
@@ -117,7 +121,7 @@ __global__ __launch_bounds__(256 * WALKS, 2 / WALKS) void attn_fwd_kernel(AttnAr
     if (kb + WALKS <= kb_last) load(kb + WALKS);  // the next key block loads while this one computes
     uint8_t* Ks = smem + (kb & kBufs) * kFwdBuf;
     uint8_t* Vs = Ks + kFwdTile;
-    if (step + WALKS > kb_mask) {
+    if constexpr (TAIL) {
       int id = tid;
       asm volatile("" : "+v"(id));  // its addresses are not kept across the loop
 #pragma unroll 1
@@ -132,7 +136,7 @@ __global__ __launch_bounds__(256 * WALKS, 2 / WALKS) void attn_fwd_kernel(AttnAr
       __syncthreads();
     }
     // A wave whose queries all precede the block has nothing to add; nor is there any past the last.
-    if (kb <= kb_last && k0 <= wq0 + 16 * QT - 1) {
+    if (!TAIL || (kb <= kb_last && k0 <= wq0 + 16 * QT - 1)) {
       f32x4 st[QT][4];  // S^T[16 tt + 4 q4 + r][query]
 #pragma unroll
       for (int c = 0; c < QT; ++c)
@@ -147,60 +151,57 @@ __global__ __launch_bounds__(256 * WALKS, 2 / WALKS) void attn_fwd_kernel(AttnAr
 #pragma unroll
           for (int c = 0; c < QT; ++c) st[c][tt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ak, qf[c][s4], st[c][tt], 0, 0, 0);
         }
-      // three K fragments stay ahead of their products
-      __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+      // five K fragments stay ahead of their products
+      __builtin_amdgcn_sched_group_barrier(0x100, 5, 0);
 #pragma unroll
-      for (int n = 0; n < 13; ++n) {
+      for (int n = 0; n < 11; ++n) {
         __builtin_amdgcn_sched_group_barrier(0x008, QT, 0);
         __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       }
-      __builtin_amdgcn_sched_group_barrier(0x008, 3 * QT, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, 5 * QT, 0);
+      if (TAIL && k0 + BLK - 1 > wq0) {  // keys past the episode come after every query of it
+#pragma unroll
+        for (int c = 0; c < QT; ++c)
+#pragma unroll
+          for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              st[c][tt][r] = k0 + 16 * tt + 4 * q4 + r <= wq0 + 16 * c + l16 ? st[c][tt][r] : -INFINITY;
+      }
       bf16x8 p[QT][2];  // weights of keys 32 u + 4 q4 .. +3 and 32 u + 16 + 4 q4 .. +3
-      // A key block that ends at or before the wave's first query is whole and entirely allowed: no mask there.
-      auto softmax = [&](auto masked) {
 #pragma unroll
-        for (int c = 0; c < QT; ++c) {
-          float mx = -INFINITY;
+      for (int c = 0; c < QT; ++c) {
+        float mx = -INFINITY;
 #pragma unroll
-          for (int tt = 0; tt < 4; ++tt)
+        for (int tt = 0; tt < 4; ++tt)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              // keys past the episode come after every query of it
-              if constexpr (decltype(masked)::value)
-                st[c][tt][r] = k0 + 16 * tt + 4 * q4 + r <= wq0 + 16 * c + l16 ? st[c][tt][r] : -INFINITY;
-              mx = fmaxf(mx, st[c][tt][r]);
-            }
-          mx = rows_max(mx) * sl;
-          if (__any(mx > m[c] + 8.0f)) {
-            const float mn = mx > m[c] + 8.0f ? mx : m[c];  // per row: no other row of the tile changes it
-            const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[c] - mn);
-            m[c] = mn;
-            l[c] *= alpha;
+          for (int r = 0; r < 4; ++r) mx = fmaxf(mx, st[c][tt][r]);
+        mx = rows_max(mx) * sl;
+        if (__any(mx > m[c] + 8.0f)) {
+          const float mn = mx > m[c] + 8.0f ? mx : m[c];  // per row: no other row of the tile changes it
+          const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m[c] - mn);
+          m[c] = mn;
+          l[c] *= alpha;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) o[c][j] *= alpha;
-          }
-          const float ms = m[c] == -INFINITY ? 0.0f : m[c];  // no key yet, or only scores of -inf: their weights are 0
-          float sum = 0.0f;
-#pragma unroll
-          for (int tt = 0; tt < 4; ++tt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              st[c][tt][r] = __builtin_amdgcn_exp2f(fmaf(st[c][tt][r], sl, -ms));
-              sum += st[c][tt][r];
-            }
-          l[c] += sum;
-#pragma unroll
-          for (int u = 0; u < 2; ++u)
-            p[c][u] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(st[c][2 * u][0], st[c][2 * u][1]),
-                                                       pack_bf16x2(st[c][2 * u][2], st[c][2 * u][3]),
-                                                       pack_bf16x2(st[c][2 * u + 1][0], st[c][2 * u + 1][1]),
-                                                       pack_bf16x2(st[c][2 * u + 1][2], st[c][2 * u + 1][3])});
+          for (int j = 0; j < 8; ++j) o[c][j] *= alpha;
         }
-      };
-      if (k0 + BLK - 1 <= wq0)
-        softmax(std::false_type{});
-      else
-        softmax(std::true_type{});
+        const float ms = m[c] == -INFINITY ? 0.0f : m[c];  // no key yet, or only scores of -inf: their weights are 0
+        float sum = 0.0f;
+#pragma unroll
+        for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            st[c][tt][r] = __builtin_amdgcn_exp2f(fmaf(st[c][tt][r], sl, -ms));
+            sum += st[c][tt][r];
+          }
+        l[c] += sum;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          p[c][u] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(st[c][2 * u][0], st[c][2 * u][1]),
+                                                     pack_bf16x2(st[c][2 * u][2], st[c][2 * u][3]),
+                                                     pack_bf16x2(st[c][2 * u + 1][0], st[c][2 * u + 1][1]),
+                                                     pack_bf16x2(st[c][2 * u + 1][2], st[c][2 * u + 1][3])});
+      }
 #pragma unroll
       for (int j = 0; j < 8; ++j)
 #pragma unroll
@@ -216,7 +217,7 @@ __global__ __launch_bounds__(256 * WALKS, 2 / WALKS) void attn_fwd_kernel(AttnAr
         __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
         __builtin_amdgcn_sched_group_barrier(0x008, QT, 0);
       }
-      if (kb >= kb_mask && found[kb & kBufs] == kb) {  // the entries taken out, for the queries that see them
+      if (TAIL && found[kb & kBufs] == kb) {  // the entries taken out, for the queries that see them
         int id = lane;
         asm volatile("" : "+v"(id));
         const bf16_t* vb = a.v + ((int64_t)(E.row0 + k0) * a.kv_heads + kh) * DH + 4 * (id >> 4);
@@ -237,7 +238,10 @@ __global__ __launch_bounds__(256 * WALKS, 2 / WALKS) void attn_fwd_kernel(AttnAr
           }
       }
     }
-  }
+  };
+  int step = 0;
+  for (; step + WALKS <= kb_mask; step += WALKS) walk_step(step, std::false_type{});
+  for (; step <= kb_last; step += WALKS) walk_step(step, std::true_type{});
   float lsum[QT];
 #pragma unroll
   for (int c = 0; c < QT; ++c) lsum[c] = rows_sum(l[c]);
@@ -317,11 +321,11 @@ static hipError_t launch_fwd(LdsLimit& limit, const AttnArgs& a, AttnBatch b, hi
 
 // One or two query tiles a wave and one or two walks, by an estimate in microseconds of the launch: starts and ends of the
 // workgroups and their steps of 64 keys, spread over the CUs, against the longest walk; the larger of the two and a part of the
-// other. Fitted to 55 shapes of 64 to 30000 rows (rms errors 7 to 9%), over which the choice takes 1.014 times the
-// best one's time on average (without two walks 1.096). One tile / two / one and two walks / two and two walks:
-// 100 rows x 16 heads 5.9 / 7.8 / 6.2 / 8.8; 4096 x 4 63 / 86 / 46 / 68; 2048 x 16 38.5 / 48.5 / 33.1 / 40.4; 8192 x 8
-// 175 / 189 / 189 / 153; 8192 x 32 658 / 525 / 738 / 575; 16 x 128 x 32 15.9 / 14.3 / 25.2 / 20.9.
-// Farthest from the best: 2 x 1000 x 32 takes 40 with the chosen two tiles, 33 with one.
+// other. Fitted to 55 shapes of 64 to 30000 rows (rms errors 7 to 8%), over which the choice takes 1.008 times the
+// best one's time on average (without two walks 1.097). One tile / two / one and two walks / two and two walks: 100
+// rows x 16 heads 5.9 / 8.6 / 6.3 / 8.6; 4096 x 4 56 / 78 / 42.5 / 60; 2048 x 16 36.0 / 44.5 / 32.2 / 36.2; 8192 x 8
+// 172 / 175 / 179 / 140; 8192 x 32 637 / 508 / 690 / 530; 16 x 128 x 32 15.6 / 14.7 / 25.1 / 20.1. Farthest from the
+// best: 2 x 1000 x 32 takes 38 with the chosen two tiles, 32 with one.
 hipError_t launch_attn_fwd(const AttnArgs& a, const AttnBatch& b, hipStream_t s) {
   static LdsLimit limits[4];
   double wgs[2] = {}, steps[2] = {}, longest = 0.0;
@@ -335,7 +339,7 @@ hipError_t launch_attn_fwd(const AttnArgs& a, const AttnBatch& b, hipStream_t s)
     double start, chain, wg, step, rest;
   };
   static constexpr Fit fits[4] = {
-      {3.95, 0.93, 2.10, 0.59, 0.14}, {5.41, 1.16, 2.40, 0.95, 0.30}, {4.97, 1.35, 4.53, 0.65, 0.0}, {7.03, 1.93, 5.84, 1.01, 0.04}};
+      {4.35, 0.77, 2.09, 0.55, 0.22}, {6.48, 1.02, 2.46, 0.91, 0.29}, {4.96, 1.22, 4.52, 0.60, 0.0}, {6.99, 1.66, 5.72, 0.93, 0.02}};
   const double cus = a.heads / 256.0;
   int best = 0;
   double least = 0.0;

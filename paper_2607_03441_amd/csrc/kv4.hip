@@ -368,7 +368,8 @@ __global__ __launch_bounds__(256, 2) void kv4_decode_kernel(Kv4Args a, Kv4Batch 
     load_k(rec);
     load_v(rec);
   }
-  for (; p < k.p1; p += 4) {
+  auto page = [&](auto masked) {
+    constexpr bool MASKED = decltype(masked)::value;
     const bool more = p + 4 < k.p1;
     const uint8_t* next = more ? record(p + 4) : rec;
     f32x4 st[8];  // S^T[16 i + 4 q4 + r][row]
@@ -381,17 +382,17 @@ __global__ __launch_bounds__(256, 2) void kv4_decode_kernel(Kv4Args a, Kv4Batch 
     }
     if (more) load_k(next);
     bf16x8 pw[4];
-    if ((int64_t)p * kPage + kPage - 1 <= all_see)
-      weigh<8, false>(st, pw, vs, sl, p * kPage + 4 * q4, lim, m, l, o);
-    else
-      weigh<8, true>(st, pw, vs, sl, p * kPage + 4 * q4, lim, m, l, o);
+    weigh<8, MASKED>(st, pw, vs, sl, p * kPage + 4 * q4, lim, m, l, o);
 #pragma unroll
     for (int j = 0; j < 8; ++j)
 #pragma unroll
       for (int u = 0; u < 4; ++u) o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(vr[j][u], 1.0f), pw[u], o[j], 0, 0, 0);
     if (more) load_v(next);
     rec = next;
-  }
+  };
+  // pages that every row sees first: masks behind a branch in one loop made the compiler copy O in every step
+  for (; p < k.p1 && (int64_t)p * kPage + kPage - 1 <= all_see; p += 4) page(std::false_type{});
+  for (; p < k.p1; p += 4) page(std::true_type{});
   // the four waves' maxima, sums and O: waves 2 and 3 hand over to 0 and 1, then 1 to 0
   __shared__ f32x4 ex[2][8][64];
   __shared__ float2 ml[2][64];
@@ -421,11 +422,10 @@ __global__ __launch_bounds__(256, 2) void kv4_decode_kernel(Kv4Args a, Kv4Batch 
 
 // Attention of 128 query rows per workgroup (prompts in chunks): every wave owns two tiles of 16 rows and goes over all
 // pages of the split, which lie in LDS as they are in the cache, the next one on its way. Nothing is joined between the waves.
-// Bound by issue: a page of 128 rows takes a wave 4 us, of which the products are a third; every wave widens all codes and
-// takes its exponentials, and two waves share a SIMD. 64 rows of 4 sequences of 512 to 8200 tokens (32 heads
-// over 8) in 39 us. With the join, when a split's row blocks were far apart: pages in each wave's registers instead of LDS
-// 80 us, this 56; two sets of four waves on alternate pages 61; one row tile a wave 57. Side by side: 50. Four row tiles a
-// wave, or fragments read a product ahead, spill.
+// Bound by issue: every wave widens all codes and takes its exponentials, and two waves share a SIMD. 64 rows of 4
+// sequences of 512 to 8200 tokens (32 heads over 8) 46 us with the join. On the way there: pages in each wave's registers
+// instead of LDS 80, here 56; two sets of four waves on alternate pages 61; one row tile a wave 57; a split's row blocks side
+// by side 50; no copies of O (see the loops) 47; V asked for before the exponentials 46. Four row tiles a wave spill.
 __global__ __launch_bounds__(256, 2) void kv4_chunk_kernel(Kv4Args a, Kv4Batch b) {
   constexpr int RT = kKv4ChunkRows / 64;
   constexpr int PT = 4;  // tiles of 16 tokens whose scores are held at a time
@@ -447,7 +447,7 @@ __global__ __launch_bounds__(256, 2) void kv4_chunk_kernel(Kv4Args a, Kv4Batch b
 #pragma unroll
     for (int j = 0; j < 8; ++j) o[c][j] = f32x4{0, 0, 0, 0};
   }
-  const int64_t all_see = k.first + row0 / k.g;  // every row of the wave sees the positions up to here
+  const int64_t all_see = k.first + k.rb * kKv4ChunkRows / k.g;  // every row of the block sees the positions up to here
   const int64_t none_see = k.first + min(row0 + 16 * RT - 1, k.S.n * k.g - 1) / k.g;  // and none those behind this
   const float sl = a.scale * kLog2e;
   const int32_t* table = a.table + (int64_t)k.S.seq * a.width;
@@ -466,14 +466,14 @@ __global__ __launch_bounds__(256, 2) void kv4_chunk_kernel(Kv4Args a, Kv4Batch b
       __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(dst + kOffKs), 16, kOffKs + lane * 16, 0, 0, 0);
   };
   if (k.p0 < k.p1) load(k.p0);
-  for (int p = k.p0; p < k.p1; ++p) {
+  auto page = [&](int p, auto masked) {
+    constexpr bool MASKED = decltype(masked)::value;
     // This wave's loads have landed; then every wave's have, and every wave is done with the other buffer.
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
     if (p + 1 < k.p1) load(p + 1);
     const uint8_t* rec = smem + (p & 1) * kChunkBuf;
-    if (!rows || (int64_t)p * kPage > none_see) continue;
-    const bool whole = (int64_t)p * kPage + kPage - 1 <= all_see;
+    if (!rows || (MASKED && (int64_t)p * kPage > none_see)) return;
     const uint2 ks = *reinterpret_cast<const uint2*>(rec + kOffKs + 128 * q4 + 8 * l16);
 #pragma unroll
     for (int h0 = 0; h0 < 8; h0 += PT) {
@@ -494,27 +494,27 @@ __global__ __launch_bounds__(256, 2) void kv4_chunk_kernel(Kv4Args a, Kv4Batch b
       u32x4 vs[PT / 2];
 #pragma unroll
       for (int i = 0; i < PT / 2; ++i) vs[i] = *reinterpret_cast<const u32x4*>(rec + kOffVs + 64 * q4 + 8 * h0 + 16 * i);
+      uint2 vr[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) vr[j] = *reinterpret_cast<const uint2*>(rec + kOffV + (16 * j + l16) * 64 + 16 * q4 + 2 * h0);
       bf16x8 pw[RT][PT / 2];
       const int t0 = p * kPage + 16 * h0 + 4 * q4;
 #pragma unroll
-      for (int c = 0; c < RT; ++c) {
-        if (whole)
-          weigh<PT, false>(st[c], pw[c], vs, sl, t0, lim[c], m[c], l[c], o[c]);
-        else
-          weigh<PT, true>(st[c], pw[c], vs, sl, t0, lim[c], m[c], l[c], o[c]);
-      }
+      for (int c = 0; c < RT; ++c) weigh<PT, MASKED>(st[c], pw[c], vs, sl, t0, lim[c], m[c], l[c], o[c]);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const uint2 vr = *reinterpret_cast<const uint2*>(rec + kOffV + (16 * j + l16) * 64 + 16 * q4 + 2 * h0);
 #pragma unroll
         for (int u = 0; u < PT / 2; ++u) {
-          const bf16x8 av = widen(u ? vr.y : vr.x, 1.0f);
+          const bf16x8 av = widen(u ? vr[j].y : vr[j].x, 1.0f);
 #pragma unroll
           for (int c = 0; c < RT; ++c) o[c][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, pw[c][u], o[c][j], 0, 0, 0);
         }
       }
     }
-  }
+  };
+  int p = k.p0;
+  for (; p < k.p1 && (int64_t)p * kPage + kPage - 1 <= all_see; ++p) page(p, std::false_type{});
+  for (; p < k.p1; ++p) page(p, std::true_type{});
   if (!rows) return;
 #pragma unroll
   for (int c = 0; c < RT; ++c)
@@ -522,8 +522,8 @@ __global__ __launch_bounds__(256, 2) void kv4_chunk_kernel(Kv4Args a, Kv4Batch b
 }
 
 // Joins the splits of a row in their order. One wave per (row, query head), two elements a lane, eight splits' loads on their
-// way. Bound by memory where there are many rows (64 x 4 rows x 32 heads, up to 13 splits: 28 MB in 8.6 us), by latency
-// otherwise (16 rows: 3.3 us).
+// way. Bound by memory where there are many rows (4 x 64 rows x 32 heads, up to 13 splits: 31 MB in 8.4 us), by latency
+// otherwise (16 rows: 3.5 us).
 __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Args a, Kv4Batch b, int64_t rows) {
   const int lane = threadIdx.x & 63, R = a.block_rows;
   const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);  // (row of the batch, head)
