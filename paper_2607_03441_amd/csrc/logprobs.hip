@@ -23,6 +23,17 @@ __device__ __forceinline__ bool better(Cand a, Cand b) { return a.z > b.z || (a.
 constexpr uint32_t kNone = 0xFFFFFFFFu;
 constexpr float kLog2e = 1.4426950408889634f;
 
+// One key per candidate, larger for the better; 0: none.
+__device__ __forceinline__ uint64_t cand_key(float z, uint32_t id) {
+  const uint32_t b = __float_as_uint(z + 0.0f);  // -0 is 0
+  return (uint64_t)(b >> 31 ? ~b : b | 0x80000000u) << 32 | ~id;
+}
+__device__ __forceinline__ Cand key_cand(uint64_t key) {
+  if (key == 0) return {-INFINITY, kNone};
+  const uint32_t b = (uint32_t)(key >> 32);
+  return {__uint_as_float(b >> 31 ? b & 0x7FFFFFFFu : ~b), ~(uint32_t)key};
+}
+
 // The best of a wave's candidates: the largest logit, then the lowest id that has it, both by exchanges within
 // rows of 16 lanes and swaps between rows (shuffles through LDS took five times as long).
 template <class T, class Op>
@@ -200,16 +211,6 @@ struct LpFusedLds {
 constexpr size_t kLpFusedLds = CfgBig::LDS + sizeof(LpFusedLds);
 static_assert(kLpFusedLds <= 160 * 1024, "LDS");
 
-__device__ __forceinline__ uint64_t cand_key(float z, uint32_t id) {
-  const uint32_t b = __float_as_uint(z + 0.0f);  // -0 is 0
-  return (uint64_t)(b >> 31 ? ~b : b | 0x80000000u) << 32 | ~id;
-}
-__device__ __forceinline__ Cand key_cand(uint64_t key) {
-  if (key == 0) return {-INFINITY, kNone};
-  const uint32_t b = (uint32_t)(key >> 32);
-  return {__uint_as_float(b >> 31 ? b & 0x7FFFFFFFu : ~b), ~(uint32_t)key};
-}
-
 template <bool TOP>
 __global__ __launch_bounds__(512) void lp_fused_kernel(LpArgs a, int tiles_t, int tiles_v) {
   using C = CfgBig;
@@ -370,11 +371,12 @@ __device__ __forceinline__ void write_top(const LpArgs& a, int64_t out, int k, C
 }
 
 // Statistics and the best `top` of 256 E logits of one staged row, E a thread, in registers; where that is all of the row,
-// the results (a joining launch as well took 4.5 us more of 30 for 512 rows of 4096). The best are drawn one after the
-// other: the best of each thread's, of each wave's, of the workgroup's; a thread keeps the best of every 16, so that a
-// draw costs its owner one scan of 16. Bound by the draws, 0.7 us each where one row is on its way, not by the
-// reads. (Waves that draw for themselves, without a barrier, and a join of their lists: 20 alternatives of
-// 4096 x 5000 logits 268 us, this 212.)
+// the results (a joining launch as well took 4.5 us more of 30 for 512 rows of 4096). A wave in which `top` lanes have a logit of
+// at least T has that many of them, so none below T is among the best: T is the top-th largest of the lanes' maxima,
+// and the largest of the four waves' holds for all. What passes, a little more than `top`, goes to LDS, and each one's place
+// is the number of those above it. Where many are equal and more than 256 pass, the best are drawn one after the other
+// instead: the best of each thread's, of each wave's, of the workgroup's; a thread keeps the best of every 16, so that
+// a draw costs its owner one scan of 16. @FIG@
 template <int E>
 __global__ __launch_bounds__(256) void lp_rows_kernel(LpArgs a) {
   constexpr int G = E / 16;
@@ -397,6 +399,7 @@ __global__ __launch_bounds__(256) void lp_rows_kernel(LpArgs a) {
       m = fmaxf(m, x[i + e]);
     }
   }
+  const float mine = m;
   m = wave_reduce(m, [](float x, float y) { return fmaxf(x, y); });
   float s = 0.0f, t = 0.0f;
   const float m0 = m == -INFINITY ? 0.0f : m, mb = m0 * kLog2e;
@@ -410,11 +413,20 @@ __global__ __launch_bounds__(256) void lp_rows_kernel(LpArgs a) {
   s = wave_reduce(s, add);
   t = wave_reduce(t, add);
   const bool all = a.splits == 1;
-  __shared__ float4 st[4];
+  __shared__ float4 st[4];  // with T
   __shared__ Cand best[2][4];
-  if (lane == 0) st[w] = make_float4(m, s, t, 0.0f);
+  __shared__ uint64_t pass[256];
+  __shared__ int passed;
+  __shared__ float lse;
+  float thr = 0.0f;
+  if (a.top > 0) {
+    int above = 0;
+    for (int j = 0; j < 64; ++j) above += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine), j)) > mine;
+    thr = wave_reduce(above < a.top ? mine : INFINITY, [](float x, float y) { return fminf(x, y); });
+  }
+  if (lane == 0) st[w] = make_float4(m, s, t, thr);
+  if (tid == 0) passed = 0;
   __syncthreads();
-  float lse = 0.0f;  // thread 0's
   if (tid == 0) {
     for (int i = 1; i < 4; ++i) stats_join(m, s, t, st[i].x, st[i].y, st[i].z);
     if (all)
@@ -423,8 +435,36 @@ __global__ __launch_bounds__(256) void lp_rows_kernel(LpArgs a) {
       a.stats[(int64_t)split * a.rows + row] = make_float4(m, s, t, zy);
   }
   if (a.top == 0) return;
-  // what is drawn, or past the row, becomes a NaN, which is better than nothing else
   auto entry = [&](int i) { return (uint32_t)(v0 + (i / 4 * 256 + tid) * 4 + (i & 3)); };
+  auto write = [&](int k, Cand c) {
+    if (all)
+      write_top(a, a.row0 + row, k, c, lse);
+    else
+      a.lists[lp_list(a, row, split, k)] = make_float2(c.z, __uint_as_float(c.id));
+  };
+  thr = fmaxf(fmaxf(st[0].w, st[1].w), fmaxf(st[2].w, st[3].w));
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < E; ++i) n += x[i] >= thr && entry(i) < (uint32_t)a.V;
+  if (n > 0) {
+    int at = atomicAdd(&passed, n);
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+      if (x[i] >= thr && entry(i) < (uint32_t)a.V) {
+        if (at < 256) pass[at] = cand_key(x[i], entry(i));
+        ++at;
+      }
+  }
+  __syncthreads();
+  n = passed;
+  if (n <= 256) {
+    const uint64_t key = tid < n ? pass[tid] : 0;
+    int place = 0;
+    for (int j = 0; j < n; ++j) place += pass[j] > key;
+    if (tid < n ? place < a.top : tid < a.top) write(tid < n ? place : tid, key_cand(key));
+    return;
+  }
+  // what is drawn, or past the row, becomes a NaN, which is better than nothing else
   auto scan = [&](int g, uint32_t drawn) {
     Cand c = {-INFINITY, kNone};
 #pragma unroll
@@ -444,7 +484,7 @@ __global__ __launch_bounds__(256) void lp_rows_kernel(LpArgs a) {
     group[g] = scan(g, kNone);
     if (better(group[g], c)) c = group[g];
   }
-  for (int n = 0; n < a.top; ++n) {
+  for (n = 0; n < a.top; ++n) {
     const Cand wb = wave_best(c);
     if (lane == 0) best[n & 1][w] = wb;
     __syncthreads();
@@ -452,12 +492,7 @@ __global__ __launch_bounds__(256) void lp_rows_kernel(LpArgs a) {
 #pragma unroll
     for (int i = 1; i < 4; ++i)
       if (better(best[n & 1][i], b)) b = best[n & 1][i];
-    if (tid == 0) {
-      if (all)
-        write_top(a, a.row0 + row, n, b, lse);
-      else
-        a.lists[lp_list(a, row, split, n)] = make_float2(b.z, __uint_as_float(b.id));
-    }
+    if (tid == 0) write(n, b);
     if (b.id != kNone && b.id == c.id) {
       c = {-INFINITY, kNone};
 #pragma unroll
