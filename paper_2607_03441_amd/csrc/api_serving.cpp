@@ -262,10 +262,11 @@ attt_status lp_check(int64_t N, int64_t d, int64_t V, int32_t dtype, int32_t top
 
 LpPlan lp_plan(int64_t N, int64_t V, int32_t dtype, int32_t top) {
   LpPlan P;
-  // Without staging a workgroup's first tile and its list cost about 50 us with alternatives, staging the writing and
-  // reading of N x V logits. Staged / not, 8 alternatives, in us: 128256 entries, 128 rows 266 / 305, 256 rows 325 / 319, 1024
-  // rows 1144 / 891; 32000 entries, 256 rows 83 / 92, 512 rows 107 / 104; 5000 entries, 512 rows 58 / 72.
-  P.fused = dtype == ATTT_BF16 && top <= kLpFusedTop && N > 128 && (top == 0 || N * V >= 10000000);
+  // Without staging a workgroup's first tile and its lists cost time that grows with the alternatives, staging the writing
+  // and reading of N x V logits. Staged / not, in us: 128256 entries, 8 alternatives, 256 rows 296 / 307, 384 rows 486 / 444,
+  // 2048 rows 2099 / 1669; 32000 entries, 8 alternatives, 512 rows 88 / 102, 2048 rows 303 / 285, 2 alternatives, 384 rows 74 /
+  // 76, 768 rows 128 / 120; without alternatives 160 rows 51 / 43; 10000 entries, 8 alternatives, 2048 rows 202 / 208.
+  P.fused = dtype == ATTT_BF16 && top <= kLpFusedTop && N > 128 && (top == 0 || N * V >= 12000000 + 3500000 * (int64_t)top);
   if (P.fused) {
     P.rows = std::min(N, kLpFusedRows);
     // Row tiles x splits workgroups, one per CU at a time: the splits with the fewest tiles one after the other, a
@@ -282,10 +283,11 @@ LpPlan lp_plan(int64_t N, int64_t V, int32_t dtype, int32_t top) {
     // rows of about 256 MiB of logits at a time
     const int64_t fit = ((int64_t)256 << 20) / (P.ldz * 4);
     P.rows = std::min<int64_t>(std::max<int64_t>(N, 1), fit >= 128 ? fit / 128 * 128 : std::max<int64_t>(1, fit));
-    // Every workgroup draws its list one by one: few long chunks where the rows fill the chip anyway and V fills the
-    // chunks. 20 alternatives with short and long chunks, in us: 128256 entries, 16 rows 218 and 224, 128 rows 308 and
-    // 294, 1024 rows 1470 and 1301; 5000 entries, 2048 rows 129 and 151.
-    P.chunk = kLpRowChunk[V >= kLpRowChunk[1] && P.rows * ceil_div(V, kLpRowChunk[0]) > 1024];
+    // Long chunks where one is the row, which then needs no joining launch, and where there are enough of them to fill the
+    // chip: fewer lists to join. 20 alternatives with short and long chunks, in us: 5000 entries, 16 rows 33 / 23;
+    // 32000 entries, 16 rows 47 / 51, 256 rows 80 / 78, 2048 rows 348 / 321; 128256 entries, 16 rows 199 / 202, 1024 rows 1115
+    // / 1072.
+    P.chunk = kLpRowChunk[V > kLpRowChunk[0] && (V <= kLpRowChunk[1] || P.rows * ceil_div(V, kLpRowChunk[0]) > 2048)];
     P.splits = (int32_t)ceil_div(V, P.chunk);
     P.block = (int32_t)P.rows;
   }

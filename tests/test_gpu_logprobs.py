@@ -94,6 +94,22 @@ def test_ties_take_the_lowest_ids(attt, N, bf16):
     compare(attt.token_logprobs(*dev(h, W, y, bf16), top=9), r, 64, True, 9)
 
 
+@pytest.mark.parametrize("N,V,top,bf16", [(3, 40000, 32, True), (3, 40000, 32, False), (5, 4000, 32, False), (300, 40000, 10, True),
+                                          (2, 1100000, 5, True), (2, 1100000, 32, False)])
+@pytest.mark.parametrize("equal", [True, False])
+def test_ties_past_every_place(attt, N, V, top, bf16, equal):
+    """All logits of a row equal, or a few values only: more candidates than are selected from at once, in any number of splits."""
+    rng = np.random.default_rng(V + top)
+    h = np.round(rng.standard_normal((N, 8)) * 16).clip(-127, 127) / 16
+    kinds = np.round(rng.standard_normal((1 if equal else 40, 8)) * 0.5 * 512).clip(-127, 127) / 512
+    W = kinds[rng.integers(0, len(kinds), V)]
+    y = rng.integers(0, V, N).astype(np.int32)
+    note(f"ties: {N} rows, {V} entries of {len(kinds)} kinds, {top} alternatives")
+    r = olp.token_logprobs(h, W, y, top)
+    # with V equal terms a sum of 64 a lane and the joins stays within the bounds' 2^-18
+    compare(attt.token_logprobs(*dev(h, W, y, bf16), top=top), r, 8, True, top)
+
+
 @pytest.mark.parametrize("N", [7, 150, 1700])
 @pytest.mark.parametrize("bf16", [True, False])
 def test_sorted_heads(attt, N, bf16):
@@ -145,6 +161,48 @@ def test_some_logits_of_minus_infinity(attt, N):
     assert np.array_equal(host(ids)[:, :20], keep[r["ids"]]) and np.array_equal(host(ids)[:, 20:], np.tile(np.arange(10, 15), (N, 1)))
     assert (np.abs(host(lp)[:, :20] - r["top"]) <= 2.0 ** -18).all() and np.isneginf(host(lp)[:, 20:]).all()
     assert (np.abs(host(ent) - r["entropy"]) <= 2.0 ** -14).all() and np.isneginf(host(logp)[0])
+
+
+@pytest.mark.parametrize("kind", ["any", "rising", "falling", "equal", "few", "nonfinite"])
+@pytest.mark.parametrize("N,V,top", [(400, 57001, 3), (5000, 9500, 10), (300, 160001, 10), (1700, 30000, 9)])
+def test_without_staged_logits(attt, N, V, top, kind):
+    """Row tiles that take what they need from logits that stay in the workgroup, against float64 on the same device."""
+    import torch
+    note(f"logprobs without staging: {N} rows, {V} entries, {top} alternatives, {kind}")
+    g = torch.Generator("cuda").manual_seed(N + top)
+    d = 64
+    h = (torch.randint(-64, 65, (N, d), generator=g, device="cuda") / 16).bfloat16()
+    W = (torch.randint(-64, 65, (V, d), generator=g, device="cuda") / 512).bfloat16()
+    if kind in ("rising", "falling"):  # every tile replaces the alternatives, or none does; steps that 8 bits hold
+        W[:, 2:] = 0
+        W[:, 0], W[:, 1] = torch.arange(V, device="cuda") * 128 // V / 512, torch.arange(V, device="cuda") % 64 / 512
+        h[:, 0], h[:, 1] = (4.0, 0.0625) if kind == "rising" else (-4.0, -0.0625)
+    elif kind in ("equal", "few"):
+        W = W[torch.randint(0, 1 if kind == "equal" else 50, (V,), generator=g, device="cuda")]
+    y = torch.randint(0, V, (N,), generator=g, device="cuda", dtype=torch.int32)
+    bad = torch.zeros(N, dtype=torch.bool, device="cuda")
+    if kind == "nonfinite":
+        h[3, 5], h[N - 1, 0], y[5], y[7] = float("nan"), float("inf"), -1, V
+        W[V - 1, 1:] = 0
+        W[V - 1, 0] = 0.0
+        bad[3] = bad[N - 1] = True
+    logp, ent, ids, lp = attt.token_logprobs(h, W, y, top=top)
+    z = h.double() @ W.double().t()
+    ref = torch.log_softmax(z, 1)
+    want = ref.gather(1, y.clamp(0, V - 1).long()[:, None])[:, 0]
+    fine = ~bad
+    if kind == "nonfinite":
+        assert torch.isnan(logp[[3, 5, 7, N - 1]]).all() and torch.isnan(ent[bad]).all()
+        assert (ids[bad] == -1).all() and torch.isnan(lp[bad]).all()
+        want[[5, 7]] = float("nan")
+    best = torch.sort(z[fine], dim=1, descending=True, stable=True)[1][:, :top]
+    assert torch.equal(ids[fine].long(), best)
+    # exact logits of at most 64 x 4 x 0.125: m - z, lse and the log-probability round by 2^-24 of up to 64 each, the sums by 2^-18
+    tol = 2.0 ** -24 * 4 * 64 + 2.0 ** -18
+    assert (lp[fine] - ref[fine].gather(1, best)).abs().max() <= tol
+    seen = fine & ~torch.isnan(want)
+    assert (logp - want)[seen].abs().max() <= tol
+    assert (ent[fine] - torch.special.entr(ref[fine].exp()).sum(1)).abs().max() <= 16 * tol
 
 
 def test_outputs_given_repeats_streams_and_graphs(attt):
