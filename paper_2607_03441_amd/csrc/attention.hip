@@ -26,6 +26,7 @@
 // significant bits): those sums mix signs (dS even sums to zero over each row), and a single
 // bf16 rounding of P or dS would show in their small elements. The final bf16 rounding of the
 // outputs is then the main error.
+#include <algorithm>
 #include <type_traits>
 
 #include "attention_core.hpp"
@@ -595,16 +596,19 @@ __global__ __launch_bounds__(256) void attn_dkdv_reduce_kernel(AttnArgs a, AttnB
 // 2140 cycles a block and workgroup at 8192 rows, 32 heads); two tiles halve them per product, and
 // halves of 32 keys, K's next block fetched in the first and V's in the second, keep that within 248
 // VGPRs without spills: 1118 -> 867 us.
-template <int QT>
-__global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a, AttnBatch b) {
+// With WALKS = 2 a second set of four waves takes the odd key blocks of the same queries, and the two sums are added through LDS.
+template <int QT, int WALKS>
+__global__ __launch_bounds__(256 * WALKS, 2 / WALKS) void attn_dq_kernel(AttnArgs a, AttnBatch b) {
   constexpr int QBLK = 64 * QT;
   int ei, h, qb;
   attn_locate(b, a.heads, true, ei, h, qb);
   const AttnEp E = b.e[ei];
   const int kh = h / (a.heads / a.kv_heads);
   const int q0 = qb * QBLK, nq = min(QBLK, E.L - q0);
-  extern __shared__ __align__(16) uint8_t smem[];  // two buffers of [K tile][V tile], [64][PR] each
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  extern __shared__ __align__(16) uint8_t lds[];
+  const int tid = threadIdx.x & 255, lane = tid & 63, w = tid >> 6;
+  const int walk = WALKS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0;
+  uint8_t* smem = lds + walk * (2 * kKvBuf);  // two buffers of [K tile][V tile], [64][PR] each
   const int l16 = lane & 15, q4 = lane >> 4;
   const int64_t qs = (int64_t)a.heads * DH, ks = (int64_t)a.kv_heads * DH;
   const int wq = 16 * QT * w;  // this wave's first query in the block
@@ -631,22 +635,24 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a, AttnBatch b
     fetch_block(f, src + ((int64_t)(E.row0 + k0) * a.kv_heads + kh) * DH, ks, nk, tid);
   };
   const int kb_last = (q0 + nq - 1) / BLK;  // the key block of the block's last query
-  fetch(a.k, 0);
-  store_block(f, kv_tile(smem, 0, 0), tid);
-  fetch(a.v, 0);
-  store_block(f, kv_tile(smem, 0, 1), tid);
-  for (int kb = 0; kb <= kb_last; ++kb) {
+  if (walk <= kb_last) {
+    fetch(a.k, walk);
+    store_block(f, kv_tile(smem, 0, 0), tid);
+    fetch(a.v, walk);
+    store_block(f, kv_tile(smem, 0, 1), tid);
+  }
+  for (int kb = walk, buf = 0; kb - walk <= kb_last; kb += WALKS, buf ^= 1) {
     const int k0 = kb * BLK;
     // This block's tiles are stored, and every wave is done with the other buffer.
     __syncthreads();
-    if (kb < kb_last) fetch(a.k, kb + 1);  // the next K block loads during the first half, V during the second
-    const bf16_t* Ks = kv_tile(smem, kb & 1, 0);
-    const bf16_t* Vs = kv_tile(smem, kb & 1, 1);
+    if (kb + WALKS <= kb_last) fetch(a.k, kb + WALKS);  // the next K block loads during the first half, V during the second
+    const bf16_t* Ks = kv_tile(smem, buf, 0);
+    const bf16_t* Vs = kv_tile(smem, buf, 1);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int ku = k0 + 32 * u;
-      // A wave whose queries all precede the half has nothing to add.
-      if (ku <= q0 + wq + 16 * QT - 1) {
+      // A wave whose queries all precede the half has nothing to add; nor is there any past the last block.
+      if (kb <= kb_last && ku <= q0 + wq + 16 * QT - 1) {
         // S^T[16 t + 4 q4 + r][query] and dP^T likewise
         f32x4 st[QT][2], dp[QT][2];
 #pragma unroll
@@ -701,11 +707,27 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a, AttnBatch b
           }
         }
       }
-      if (kb < kb_last) {
-        store_block(f, kv_tile(smem, (kb + 1) & 1, u), tid);
-        if (u == 0) fetch(a.v, kb + 1);
+      if (kb + WALKS <= kb_last) {
+        store_block(f, kv_tile(smem, buf ^ 1, u), tid);
+        if (u == 0) fetch(a.v, kb + WALKS);
       }
     }
+  }
+  if constexpr (WALKS > 1) {
+    f32x4(*ex)[QT][8][64] = reinterpret_cast<f32x4(*)[QT][8][64]>(lds);
+    __syncthreads();
+    if (walk) {
+#pragma unroll
+      for (int c = 0; c < QT; ++c)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) ex[w][c][j][lane] = dq[c][j];
+    }
+    __syncthreads();
+    if (walk) return;
+#pragma unroll
+    for (int c = 0; c < QT; ++c)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) dq[c][j] += ex[w][c][j][lane];
   }
   // D of dQ tile j: lane (l16, q4), register r -> query 16 c + 4 q4 + r of the wave's, column 16 j + l16
 #pragma unroll
@@ -720,10 +742,10 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnArgs a, AttnBatch b
     }
 }
 
-// A kernel whose 256-thread workgroups take blocks of `rows` queries or keys of one of `heads`.
+// A kernel whose workgroups take blocks of `rows` queries or keys of one of `heads`.
 template <class K>
 static hipError_t launch_blocks(K kernel, LdsLimit& limit, int rows, int heads, size_t lds, const AttnArgs& a, AttnBatch b,
-                                int id, hipStream_t s) {
+                                int id, hipStream_t s, int threads = 256) {
   if (hipError_t e = limit.raise((const void*)kernel, lds)) return e;
   int n = 0;
   for (int i = 0; i < b.count; ++i) {
@@ -733,7 +755,7 @@ static hipError_t launch_blocks(K kernel, LdsLimit& limit, int rows, int heads, 
   }
   if (n <= 0) return hipSuccess;
   KernelTimer t(id, s);
-  hipLaunchKernelGGL(kernel, dim3(n), dim3(256), lds, s, a, b);
+  hipLaunchKernelGGL(kernel, dim3(n), dim3(threads), lds, s, a, b);
   return hipGetLastError();
 }
 
@@ -762,7 +784,7 @@ static hipError_t launch_keys(LdsLimit& limit, const AttnArgs& a, AttnBatch b, h
 }
 
 hipError_t launch_attn(int kernel, const AttnArgs& a, const AttnBatch& b, hipStream_t s) {
-  static LdsLimit limits[7];
+  static LdsLimit limits[8];
   if (kernel == 1 && b.tiles == 0)
     return launch_blocks(attn_dkdv_short_kernel, limits[6], BLK, a.kv_heads, 2 * (size_t)kQoBuf, a, b, K_ATTN_DKDV, s);
   if (kernel == 1) return b.tiles == 1 ? launch_keys<1>(limits[4], a, b, s) : launch_keys<2>(limits[5], a, b, s);
@@ -773,14 +795,22 @@ hipError_t launch_attn(int kernel, const AttnArgs& a, const AttnBatch& b, hipStr
   // two-tile workgroups: 256 (2048 rows x 16 heads) 51 + 61 / 63 + 71 us; 416 (6636 x 8) 169 + 220 / 203 + 244; 456
   // (6540 x 8 and three short ones) 151 + 195 / 190 + 225; 504 (9 of 781 x 8) 42 + 50 / 36 + 44; 720 (4518 x 20)
   // 190 + 237 / 143 + 190; 768 (3 of 3970 x 8) 196 + 241 / 157 + 216; 2048 of either (64 of 64 x 32) 32 + 39 / 35 + 41.
-  int n1 = 0, n2 = 0;
-  for (int i = 0; i < b.count; ++i) n1 += (b.e[i].L + 63) / 64, n2 += (b.e[i].L + 127) / 128;
+  int n1 = 0, n2 = 0, longest = 0;
+  for (int i = 0; i < b.count; ++i) {
+    n1 += (b.e[i].L + 63) / 64, n2 += (b.e[i].L + 127) / 128;
+    longest = std::max(longest, (b.e[i].L + 63) / 64);
+  }
   const bool wide = (int64_t)n2 * a.heads > 480 && 8 * (int64_t)n1 > 9 * (int64_t)n2;
   if (kernel == 0)
     return wide ? launch_blocks(attn_fwd_stats_kernel<2>, limits[0], 128, a.heads, lds, a, b, K_ATTN_FWD, s)
                 : launch_blocks(attn_fwd_stats_kernel<1>, limits[1], 64, a.heads, lds, a, b, K_ATTN_FWD, s);
-  return wide ? launch_blocks(attn_dq_kernel<2>, limits[2], 128, a.heads, lds, a, b, K_ATTN_DQ, s)
-              : launch_blocks(attn_dq_kernel<1>, limits[3], 64, a.heads, lds, a, b, K_ATTN_DQ, s);
+  // Two walks, where the backward is given the forward's output, for few long walks: dQ with one / two, us: 512 workgroups of
+  // up to 32 blocks (2048 rows x 16 heads) 68 / 53, of 64 (4096 x 8) 121 / 91, 256 of 8 (512 x 32) 22 / 18, but of 2 (16 x 128
+  // x 16) 14 / 19; 384 of 8 (6 x 512 x 8) 26 / 26; 1024 of 32 (2048 x 32) 90 / 97; 832 of 104 (6636 x 8) 206 / 223.
+  if (a.o && (int64_t)n1 * a.heads <= 512 && longest > 4)
+    return launch_blocks(attn_dq_kernel<1, 2>, limits[7], 64, a.heads, 2 * lds, a, b, K_ATTN_DQ, s, 512);
+  return wide ? launch_blocks(attn_dq_kernel<2, 1>, limits[2], 128, a.heads, lds, a, b, K_ATTN_DQ, s)
+              : launch_blocks(attn_dq_kernel<1, 1>, limits[3], 64, a.heads, lds, a, b, K_ATTN_DQ, s);
 }
 
 }  // namespace attt

@@ -236,6 +236,12 @@ def test_saved_backward(attt, H, kv, off):
     assert alone[3].equal(dsum)
 
 
+@pytest.mark.parametrize("H,kv,off", [(2, 1, [0, 1, 900, 901, 1700]), (8, 4, [0, 640, 961]), (3, 3, [0, 321])])
+def test_saved_backward_of_long_walks(attt, H, kv, off):
+    """Few workgroups of more than four key blocks, an odd and an even number of them: two sets of waves share the walks."""
+    test_saved_backward(attt, H, kv, off)
+
+
 def test_gradient_against_differences(attt):
     """Central differences of sum(dout * O) in float64 along random directions, for inputs that bf16 holds."""
     off = np.array([0, 33, 100], np.int64)
