@@ -635,24 +635,24 @@ __global__ __launch_bounds__(256 * WALKS, 2 / WALKS) void attn_dq_kernel(AttnArg
     fetch_block(f, src + ((int64_t)(E.row0 + k0) * a.kv_heads + kh) * DH, ks, nk, tid);
   };
   const int kb_last = (q0 + nq - 1) / BLK;  // the key block of the block's last query
-  if (walk <= kb_last) {
+  if (WALKS == 1 || walk <= kb_last) {
     fetch(a.k, walk);
     store_block(f, kv_tile(smem, 0, 0), tid);
     fetch(a.v, walk);
     store_block(f, kv_tile(smem, 0, 1), tid);
   }
-  for (int kb = walk, buf = 0; kb - walk <= kb_last; kb += WALKS, buf ^= 1) {
-    const int k0 = kb * BLK;
+  for (int step = 0; step <= kb_last; step += WALKS) {
+    const int kb = step + walk, k0 = kb * BLK;
     // This block's tiles are stored, and every wave is done with the other buffer.
     __syncthreads();
     if (kb + WALKS <= kb_last) fetch(a.k, kb + WALKS);  // the next K block loads during the first half, V during the second
-    const bf16_t* Ks = kv_tile(smem, buf, 0);
-    const bf16_t* Vs = kv_tile(smem, buf, 1);
+    const bf16_t* Ks = kv_tile(smem, kb / WALKS & 1, 0);
+    const bf16_t* Vs = kv_tile(smem, kb / WALKS & 1, 1);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int ku = k0 + 32 * u;
       // A wave whose queries all precede the half has nothing to add; nor is there any past the last block.
-      if (kb <= kb_last && ku <= q0 + wq + 16 * QT - 1) {
+      if ((WALKS == 1 || kb <= kb_last) && ku <= q0 + wq + 16 * QT - 1) {
         // S^T[16 t + 4 q4 + r][query] and dP^T likewise
         f32x4 st[QT][2], dp[QT][2];
 #pragma unroll
@@ -708,7 +708,7 @@ __global__ __launch_bounds__(256 * WALKS, 2 / WALKS) void attn_dq_kernel(AttnArg
         }
       }
       if (kb + WALKS <= kb_last) {
-        store_block(f, kv_tile(smem, buf ^ 1, u), tid);
+        store_block(f, kv_tile(smem, (kb / WALKS + 1) & 1, u), tid);
         if (u == 0) fetch(a.v, kb + WALKS);
       }
     }
