@@ -86,12 +86,15 @@ Kv4Plan kv4_plan(const Rows& rows, int32_t E, int32_t heads, int32_t kv_heads, i
   // long as six to eight of 16. By 16 / by 128 in us, 32 heads over 8: 8 sequences of 65536 tokens, 5 rows 148 / 217,
   // 24 rows 318 / 318, 56 rows 690 / 610, 128 rows 1414 / 1209; 16 of 4096, 56 rows 89 / 99, 256 rows 386 / 286; 15 of 4000
   // with one row and one of 2000 with 512 55 / 65.
-  // Workgroups of 16 rows take four pages at a time, one a wave: eight at least, so that each has one on its way (four: 16
-  // rows over 4000 tokens 31 us with the append, eight 28). Splits so that the wanted workgroups come about, which fills the
+  // Workgroups of 16 rows take four pages at a time, one a wave: eight at least, so that each has one on its way and up to
+  // eight pages need no join, but four where that makes at most one workgroup a CU and 32 splits to join. Eight / four, in us:
+  // one row of 32 heads over 8, 1024 tokens 8.0 / 9.0, 4096 10.8 / 9.1, 16384 11.3 / 10.3, 32768 14.4 / 16.2; 4 rows over 4096
+  // 11.2 / 9.3, 8 13.2 / 13.2; 16 uneven ones 21.2 / 23.1 with the append; one of 8 heads over 1, 131072 tokens 19.5 / 26.6. Splits so that the wanted workgroups come about, which fills the
   // chip where the sequences are uneven; more cost more in the join. In us, wanted 1024 / 2048 / 4096 / 8192: 8
   // rows over up to 131072 tokens 150 / 139 / 143 / 158. Blocks of 128 rows, 512 / 768 / 1024 / 1536 / 2048: 4 x 64 rows
   // over up to 8200 tokens 67 / 54 / 50 / 60 / 61 (now 46).
-  const int64_t step = P.block_rows == 16 ? 8 : 1, wanted = P.block_rows == 16 ? 2048 : 1024;
+  const int64_t step = P.block_rows != 16 ? 1 : pages > 8 && pages <= 128 && pages * P.units <= 1024 ? 4 : 8;
+  const int64_t wanted = P.block_rows == 16 ? 2048 : 1024;
   const int64_t chunk = std::max(step, round_up(ceil_div(pages * P.units, wanted), step));
   P.chunk = (int32_t)std::min(chunk, round_up(pages, step));
   P.splits = (int32_t)ceil_div(pages, P.chunk);
