@@ -521,13 +521,16 @@ __global__ __launch_bounds__(256, 2) void kv4_chunk_kernel(Kv4Args a, Kv4Batch b
     write_rows(a, k, 16 * RT * w + 16 * c + l16, m[c], bad ? __uint_as_float(0x7FC00000u) : rows_sum(l[c]), o[c], q4);
 }
 
-// Joins the splits of a row in their order. One wave per (row, query head), two elements a lane, eight splits' loads on their
-// way. Bound by memory where there are many rows (4 x 64 rows x 32 heads, up to 13 splits: 31 MB in 8.4 us), by latency
-// otherwise (16 rows: 3.5 us).
+// Joins the splits of a row in their order. W waves per (row, query head), each a range of the splits, two elements a lane,
+// eight splits' loads on their way. Bound by memory where there are many rows (4 x 64 rows x 32 heads, up to 13 splits: 31 MB in
+// 8.4 us), by latency otherwise (16 rows: 3.5 us). Four waves where the splits are many and the rows few, attention and
+// join with one / four: one row of 32 heads, 16 splits 9.4 / 9.9, 64 splits 23.1 / 20.7; 8 heads, 128 splits 19.2 / 13.3; the 8192
+// (row, head) above 46 / 58.
+template <int W>
 __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Args a, Kv4Batch b, int64_t rows) {
-  const int lane = threadIdx.x & 63, R = a.block_rows;
-  const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);  // (row of the batch, head)
-  if (at >= rows * a.heads) return;
+  const int lane = threadIdx.x & 63, R = a.block_rows, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t at = (int64_t)blockIdx.x * (4 / W) + w / W;  // (row of the batch, head)
+  if (W == 1 && at >= rows * a.heads) return;
   const int64_t row = b.s[0].row0 + at / a.heads;
   const int h = (int)(at % a.heads), g = a.heads / a.kv_heads;
   // rows of empty sequences do not exist, so the last sequence that begins at or before the row holds it
@@ -541,8 +544,9 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Args a, Kv4Batch b, in
   const int64_t unit = ((int64_t)(S.blk0 + r / R) * a.kv_heads + h / g) * a.splits;
   float m = -INFINITY, l = 0.0f;
   float2 o = make_float2(0.0f, 0.0f);
-  for (int s0 = 0; s0 < ns; s0 += 64) {  // a lane's factor is that of split s0 + lane
-    const int n = __builtin_amdgcn_readfirstlane(min(64, ns - s0));
+  const int each = (ns + W - 1) / W, end = min(ns, (w % W + 1) * each);
+  for (int s0 = w % W * each; s0 < end; s0 += 64) {  // a lane's factor is that of split s0 + lane
+    const int n = __builtin_amdgcn_readfirstlane(min(64, end - s0));
     const int64_t u = (unit + s0) * R + r % R;
     const float2 ml = lane < n ? a.part_ml[u + (int64_t)lane * R] : make_float2(-INFINITY, 0.0f);
     const float mn = fmaxf(m, wave_max(ml.x)), ms = mn == -INFINITY ? 0.0f : mn;
@@ -562,6 +566,25 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Args a, Kv4Batch b, in
         o.x = fmaf(x[i].x, fs, o.x);
         o.y = fmaf(x[i].y, fs, o.y);
       }
+    }
+  }
+  if constexpr (W > 1) {
+    __shared__ float2 ml[W], ox[W][64];
+    if (lane == 0) ml[w] = make_float2(m, l);
+    ox[w][lane] = o;
+    __syncthreads();
+    if (w > 0) return;
+#pragma unroll
+    for (int i = 1; i < W; ++i) m = fmaxf(m, ml[i].x);
+    const float ms = m == -INFINITY ? 0.0f : m;
+    l = 0.0f;
+    o = make_float2(0.0f, 0.0f);
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      const float f = __builtin_amdgcn_exp2f(ml[i].x - ms);
+      l = fmaf(ml[i].y, f, l);
+      o.x = fmaf(ox[i][lane].x, f, o.x);
+      o.y = fmaf(ox[i][lane].y, f, o.y);
     }
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
@@ -602,7 +625,10 @@ static hipError_t launch_blocks(K kernel, LdsLimit& limit, size_t lds, const Kv4
   }
   if (a.splits > 1) {
     KernelTimer t(K_KV4_JOIN, s);
-    hipLaunchKernelGGL(kv4_join_kernel, dim3((unsigned)((rows * a.heads + 3) / 4)), dim3(256), 0, s, a, b, rows);
+    if (a.splits > 16 && rows * a.heads <= 1024)
+      hipLaunchKernelGGL(kv4_join_kernel<4>, dim3((unsigned)(rows * a.heads)), dim3(256), 0, s, a, b, rows);
+    else
+      hipLaunchKernelGGL(kv4_join_kernel<1>, dim3((unsigned)((rows * a.heads + 3) / 4)), dim3(256), 0, s, a, b, rows);
   }
   return hipGetLastError();
 }

@@ -220,6 +220,17 @@ def test_row_blocks_beside_each_other(attt, lengths, rows, H, kv):
     check_attention(s, want, o, lse)
 
 
+@pytest.mark.parametrize("lengths,rows,H,kv", [([20000, 0, 130, 9000], [1, 1, 1, 2], 4, 1), ([12345], [1], 2, 2), ([9000, 100], [3, 3], 4, 4)])
+def test_few_rows_of_long_sequences(attt, lengths, rows, H, kv):
+    """Many splits of few rows, short and idle sequences beside them: four waves join a row's."""
+    s = make(lengths, rows, H, kv, 90 + sum(rows))
+    note(f"kv4 many splits: lengths {lengths}, new rows {rows}, {H} heads over {kv}")
+    cache, _, _, o, lse = run(attt, s, max_length=max(lengths))
+    want, _, _ = expected(s)
+    assert np.array_equal(cache, want)
+    check_attention(s, want, o, lse)
+
+
 def test_no_pages(attt):
     """A cache without a page: only sequences without a token have a result. The calls with any are refused or NaN."""
     import ctypes
