@@ -246,7 +246,8 @@ constexpr int64_t kLpFusedRows = 65536;   // rows of a launch without staging, w
 struct LpPlan {
   bool fused = false;          // no staged logits
   int64_t ldz = 0, rows = 0;   // staged logits: row length; rows at a time
-  int32_t splits = 0, block = 0, chunk = 0;
+  int32_t splits = 0, block = 0, chunk = 0, parts = 1;
+  bool small_tiles = false;
   size_t off_stats = 0, off_lists = 0, total = 0;
   bool joined() const { return fused || splits > 1; }  // rows of one staged chunk are finished at once
 };
@@ -263,13 +264,15 @@ attt_status lp_check(int64_t N, int64_t d, int64_t V, int32_t dtype, int32_t top
   return ATTT_OK;
 }
 
-LpPlan lp_plan(int64_t N, int64_t V, int32_t dtype, int32_t top) {
+LpPlan lp_plan(int64_t N, int64_t d, int64_t V, int32_t dtype, int32_t top) {
   LpPlan P;
   // Without staging a workgroup's first tile and its lists cost time that grows with the alternatives, staging the writing
   // and reading of N x V logits. Staged / not, in us: 128256 entries, 8 alternatives, 256 rows 296 / 307, 384 rows 486 / 444,
   // 2048 rows 2099 / 1669; 32000 entries, 8 alternatives, 512 rows 88 / 102, 2048 rows 303 / 285, 2 alternatives, 384 rows 74 /
-  // 76, 768 rows 128 / 120; without alternatives 160 rows 51 / 43; 10000 entries, 8 alternatives, 2048 rows 202 / 208.
-  P.fused = dtype == ATTT_BF16 && top <= kLpFusedTop && N > 128 && (top == 0 || N * V >= 12000000 + 3500000 * (int64_t)top);
+  // 76, 768 rows 128 / 120; 10000 entries, 8 alternatives, 2048 rows 202 / 208. Without alternatives the tiles have to fill
+  // half the chip: 10000 entries, d 4096, 160 rows 43 / 73, 512 rows 64 / 76, 1024 rows 93 / 79.
+  P.fused = dtype == ATTT_BF16 && top <= kLpFusedTop && N > 128 &&
+            (top == 0 ? ceil_div(N, 256) * ceil_div(V, 256) >= 128 : N * V >= 12000000 + 3500000 * (int64_t)top);
   if (P.fused) {
     P.rows = std::min(N, kLpFusedRows);
     // Row tiles x splits workgroups, one per CU at a time: the splits with the fewest tiles one after the other, a
@@ -293,8 +296,20 @@ LpPlan lp_plan(int64_t N, int64_t V, int32_t dtype, int32_t top) {
     P.chunk = kLpRowChunk[V > kLpRowChunk[0] && (V <= kLpRowChunk[1] || P.rows * ceil_div(V, kLpRowChunk[0]) > 2048)];
     P.splits = (int32_t)ceil_div(V, P.chunk);
     P.block = (int32_t)P.rows;
+    if (dtype == ATTT_BF16) {
+      // Tiles of 128 where those of 256 fill less than half the chip, and then the products over parts of d, at least 1024
+      // of it, which the row kernel adds: a workgroup's walk over d is a chain of loads. Without / with, 12 alternatives, in us:
+      // 2000 entries, d 4096, 1 row 44 / 21, 256 rows 82 / 26; 10000 entries, d 4096, 16 rows 51 / 36, 512 rows 92 / 72; 20000
+      // entries, d 5120, 1 row 66 / 46. Parts of 256: 10000 entries, d 1024, 16 rows 22 / 27.
+      const int64_t small = ceil_div(V, 128) * ceil_div(P.rows, 128), big = ceil_div(V, 256) * ceil_div(P.rows, 256);
+      P.small_tiles = P.rows <= 128 || big < 128;
+      if (P.small_tiles && P.rows == N) {
+        const int64_t steps = ceil_div(d, 64), parts = std::max<int64_t>(1, std::min<int64_t>({8, steps / 16, 512 / small}));
+        P.parts = (int32_t)ceil_div(steps, ceil_div(steps, parts));
+      }
+    }
   }
-  P.off_stats = align256((size_t)P.rows * P.ldz * 4);
+  P.off_stats = align256((size_t)P.rows * P.ldz * 4 * P.parts);
   P.off_lists = P.off_stats + (P.joined() ? align256((size_t)P.rows * P.splits * sizeof(float4)) : 0);
   P.total = P.off_lists + (top > 0 && P.joined() ? align256((size_t)round_up(P.rows, P.block) * P.splits * top * sizeof(float2)) : 0);
   return P;
@@ -306,7 +321,7 @@ extern "C" attt_status attt_logprobs_workspace_size(int64_t N, int64_t d, int64_
   if (!bytes) return fail(ATTT_EINVAL, "logprobs: bytes is null");
   attt_status st = lp_check(N, d, V, dtype, top);
   if (st) return st;
-  *bytes = lp_plan(N, V, dtype, top).total;
+  *bytes = lp_plan(N, d, V, dtype, top).total;
   return ATTT_OK;
 }
 
@@ -321,7 +336,7 @@ extern "C" attt_status attt_token_logprobs(const void* hidden, const void* lm_he
   if (top > 0 && (!top_ids || !top_logp)) return fail(ATTT_EINVAL, "logprobs: null pointer");
   if (!aligned16(hidden) || !aligned16(lm_head))
     return fail(ATTT_EINVAL, "logprobs: hidden and lm_head must be 16-byte aligned");
-  const LpPlan P = lp_plan(N, V, dtype, top);
+  const LpPlan P = lp_plan(N, d, V, dtype, top);
   if (workspace_bytes < P.total) return fail(ATTT_ENOSPACE, "logprobs: workspace %zu bytes, need %zu", workspace_bytes, P.total);
   if (!workspace) return fail(ATTT_EINVAL, "logprobs: workspace is null");
   if (!aligned256(workspace)) return fail(ATTT_EINVAL, "logprobs: workspace must be 256-byte aligned");
@@ -344,6 +359,8 @@ extern "C" attt_status attt_token_logprobs(const void* hidden, const void* lm_he
   a.splits = P.splits;
   a.block = P.block;
   a.chunk = P.chunk;
+  a.parts = P.parts;
+  a.small_tiles = P.small_tiles;
   hipStream_t s = static_cast<hipStream_t>(stream);
   for (int64_t r0 = 0; r0 < N; r0 += P.rows) {
     a.row0 = (int32_t)r0;

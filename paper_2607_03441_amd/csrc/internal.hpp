@@ -252,6 +252,8 @@ struct LpArgs {
   int32_t N, d, V, top;
   int32_t row0, rows;    // the rows of the launch
   int32_t splits, block, chunk;
+  int32_t parts;         // staged logits are the sum of this many slabs [rows][ldz], each over a part of d
+  bool small_tiles;      // bf16: 128 x 128 tiles
 };
 hipError_t launch_lp_logits(int dtype, const LpArgs& a, hipStream_t s);
 // bf16, top <= kLpFusedTop: statistics and lists of `splits` parts of the vocabulary, without staged logits

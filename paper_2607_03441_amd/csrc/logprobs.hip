@@ -81,19 +81,22 @@ __device__ __forceinline__ void stats_join(float& m, float& s, float& t, float m
 }
 }  // namespace
 
-// Logits of 128 vocabulary entries x 128 rows, transposed as in the cross-entropy's forward: a lane holds
+// Logits of 128 vocabulary entries x 128 rows over a part of d, transposed as in the cross-entropy's forward: a lane holds
 // groups of four consecutive entries of its row. Bound by the head's bytes: 16 rows, 128256 x 4096, 1.05 GB in 168 us, 6.2
 // TB/s; a library product of the shape takes 186.
 __global__ __launch_bounds__(256) void lp_logits_bf16_kernel(LpArgs a, int tiles_v, int tiles_t) {
   using C = CfgSmall;
   extern __shared__ __align__(16) uint8_t smem[];
+  const int tiles = tiles_v * tiles_t, part = blockIdx.x / tiles;
   int tv, tt;
-  tile_of(blockIdx.x, tiles_v, tiles_t, tv, tt);
+  tile_of(blockIdx.x - part * tiles, tiles_v, tiles_t, tv, tt);
   const int v0 = tv * C::BM, t0 = tt * C::BN;
+  const int each = ((a.d + 63) / 64 + a.parts - 1) / a.parts * 64, k0 = part * each;
   f32x16 acc[C::TM][C::TN];
-  mfma_mainloop<C>(static_cast<const bf16_t*>(a.W) + (int64_t)v0 * a.d, a.d, a.V - v0,
-                   static_cast<const bf16_t*>(a.h) + (int64_t)(a.row0 + t0) * a.d, a.d, a.rows - t0, a.d,
+  mfma_mainloop<C>(static_cast<const bf16_t*>(a.W) + (int64_t)v0 * a.d + k0, a.d, a.V - v0,
+                   static_cast<const bf16_t*>(a.h) + (int64_t)(a.row0 + t0) * a.d + k0, a.d, a.rows - t0, min(each, a.d - k0),
                    reinterpret_cast<bf16_t*>(smem), acc);
+  float* logits = a.logits + (int64_t)part * a.rows * a.ldz;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int wm = wave / C::WGN, wn = wave % C::WGN;
 #pragma unroll
@@ -106,13 +109,13 @@ __global__ __launch_bounds__(256) void lp_logits_bf16_kernel(LpArgs a, int tiles
       for (int r = 0; r < 16; r += 4) {
         const int v = v0 + wm * C::WTM + i * 32 + mfma_row(r, lane);
         if (v < a.V)  // ldz is a multiple of 4: a group that begins inside the row ends in its padding
-          *reinterpret_cast<f32x4*>(a.logits + (int64_t)t * a.ldz + v) =
+          *reinterpret_cast<f32x4*>(logits + (int64_t)t * a.ldz + v) =
               f32x4{acc[i][j][r], acc[i][j][r + 1], acc[i][j][r + 2], acc[i][j][r + 3]};
       }
   }
 }
 
-// The same with 256 x 256 tiles on eight waves, for more than 128 rows.
+// The same with 256 x 256 tiles on eight waves, for more rows.
 __global__ __launch_bounds__(512) void lp_logits_big_kernel(LpArgs a, int tiles_v, int tiles_t) {
   using C = CfgBig;
   extern __shared__ __align__(16) uint8_t smem[];
@@ -386,19 +389,30 @@ __global__ __launch_bounds__(256) void lp_rows_kernel(LpArgs a) {
   const float* z = a.logits + (int64_t)row * a.ldz;
   const int v0 = split * (256 * E);
   const int y = a.labels[a.row0 + row];
-  const float zy = y >= v0 && y < min(a.V, v0 + 256 * E) ? z[y] : __uint_as_float(0x7FC00000u);
+  const int64_t slab = (int64_t)a.rows * a.ldz;
+  float zy = __uint_as_float(0x7FC00000u);
+  if (y >= v0 && y < min(a.V, v0 + 256 * E)) {
+    zy = z[y];
+    for (int k = 1; k < a.parts; ++k) zy += z[k * slab + y];
+  }
+  f32x4 four[E / 4];
+#pragma unroll
+  for (int i = 0; i < E / 4; ++i) {
+    const int v = v0 + (i * 256 + tid) * 4;
+    four[i] = v < a.V ? *reinterpret_cast<const f32x4*>(z + v) : f32x4{0, 0, 0, 0};
+  }
+  for (int k = 1; k < a.parts; ++k)
+#pragma unroll
+    for (int i = 0; i < E / 4; ++i) {
+      const int v = v0 + (i * 256 + tid) * 4;
+      if (v < a.V) four[i] += *reinterpret_cast<const f32x4*>(z + k * slab + v);
+    }
   float x[E];  // entry i: v0 + (i / 4 * 256 + tid) * 4 + i % 4; past the row -inf
   float m = -INFINITY;
 #pragma unroll
-  for (int i = 0; i < E; i += 4) {
-    const int v = v0 + (i / 4 * 256 + tid) * 4;
-    f32x4 four = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-    if (v < a.V) four = *reinterpret_cast<const f32x4*>(z + v);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      x[i + e] = v + e < a.V ? four[e] : -INFINITY;
-      m = fmaxf(m, x[i + e]);
-    }
+  for (int i = 0; i < E; ++i) {
+    x[i] = v0 + (i / 4 * 256 + tid) * 4 + i % 4 < a.V ? four[i / 4][i % 4] : -INFINITY;
+    m = fmaxf(m, x[i]);
   }
   const float mine = m;
   m = wave_reduce(m, [](float x, float y) { return fmaxf(x, y); });
@@ -586,7 +600,7 @@ __global__ __launch_bounds__(256) void lp_join_kernel(LpArgs a) {
 
 hipError_t launch_lp_logits(int dtype, const LpArgs& a, hipStream_t s) {
   KernelTimer t(K_LP_LOGITS, s);
-  if (dtype == 1 && a.rows > 128) {
+  if (dtype == 1 && !a.small_tiles) {
     static LdsLimit limit;
     if (hipError_t e = limit.raise((const void*)lp_logits_big_kernel, CfgBig::LDS)) return e;
     const int tv = (a.V + 255) / 256, tt = (a.rows + 255) / 256;
@@ -595,7 +609,7 @@ hipError_t launch_lp_logits(int dtype, const LpArgs& a, hipStream_t s) {
     static LdsLimit limit;
     if (hipError_t e = limit.raise((const void*)lp_logits_bf16_kernel, CfgSmall::LDS)) return e;
     const int tv = (a.V + CfgSmall::BM - 1) / CfgSmall::BM, tt = (a.rows + CfgSmall::BN - 1) / CfgSmall::BN;
-    hipLaunchKernelGGL(lp_logits_bf16_kernel, dim3(tv * tt), dim3(256), CfgSmall::LDS, s, a, tv, tt);
+    hipLaunchKernelGGL(lp_logits_bf16_kernel, dim3(tv * tt * a.parts), dim3(256), CfgSmall::LDS, s, a, tv, tt);
   } else {
     const int tv = (a.V + 63) / 64, tt = (a.rows + 63) / 64;
     hipLaunchKernelGGL(lp_logits_f32_kernel, dim3(tv * tt), dim3(256), 0, s, a, tt);

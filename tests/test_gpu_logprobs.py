@@ -205,6 +205,18 @@ def test_without_staged_logits(attt, N, V, top, kind):
     assert (ent[fine] - torch.special.entr(ref[fine].exp()).sum(1)).abs().max() <= 16 * tol
 
 
+@pytest.mark.parametrize("N,d,V,top", [(1, 2048, 3000, 5), (9, 4104, 700, 3), (130, 4096, 2000, 12), (200, 3080, 20001, 0), (128, 8192, 130, 32),
+                                       (300, 2056, 17000, 4)])
+def test_parts_of_d(attt, N, d, V, top):
+    """Few tiles of a long contraction: its parts are products of their own, the last one ragged."""
+    note(f"logprobs in parts: {N} rows of {d}, {V} entries, {top} alternatives")
+    h, W, y = grid(N, d, V, 23 + V, lean=False)
+    W[:, 64:] = np.where(np.arange(64, d) % 7 == 0, W[:, 64:], 0.0)  # logits exact in any order: at most 2^24 steps of 2^-13
+    y[-1] = V  # no such entry
+    r = olp.token_logprobs(h, W, y, top)
+    compare(attt.token_logprobs(*dev(h, W, y, True), top=top), r, d, True, top)
+
+
 def test_outputs_given_repeats_streams_and_graphs(attt):
     import torch
     for N, bf16 in ((16, True), (200, True), (70, False)):
