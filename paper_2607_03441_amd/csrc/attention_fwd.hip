@@ -271,19 +271,26 @@ __global__ __launch_bounds__(256 * WALKS, 2 / WALKS) void attn_fwd_kernel(AttnAr
       for (int j = 0; j < 8; ++j) o[c][j] = o[c][j] * fa + ex[w][c][j][lane] * fb;
     }
   }
+  // O goes through LDS, chunk c of row r at place c ^ (r % 16), so that whole rows are stored: by a place of its own for each
+  // wave, in a buffer that nobody reads any more.
+  uint8_t* rows = smem + (WALKS > 1 ? 3 : (kb_last + 1) & 1) * kFwdBuf + w * (16 * QT * DH * 2);
+  static_assert(4 * 16 * QT * DH * 2 <= kFwdBuf && (WALKS == 1 || 4 * QT * (8 * 64 * 16 + 64 * 8) <= 3 * kFwdBuf), "LDS");
 #pragma unroll
   for (int c = 0; c < QT; ++c) {
     const int qry = 16 * QT * w + 16 * c + l16;
     const float lc = lsum[c];
-    if (qry < nq) {
-      if (q4 == 0) a.lse[(int64_t)h * a.N + E.row0 + q0 + qry] = m[c] / kLog2e + logf(lc);
-      const float inv = 1.0f / lc;
-      bf16_t* orow = a.o + ((int64_t)(E.row0 + q0 + qry) * a.heads + h) * DH;
+    if (q4 == 0 && qry < nq) a.lse[(int64_t)h * a.N + E.row0 + q0 + qry] = m[c] / kLog2e + logf(lc);
+    const float inv = 1.0f / lc;
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        *reinterpret_cast<uint2*>(orow + 16 * j + 4 * q4) =
-            make_uint2(pack_bf16x2(o[c][j][0] * inv, o[c][j][1] * inv), pack_bf16x2(o[c][j][2] * inv, o[c][j][3] * inv));
-    }
+    for (int j = 0; j < 8; ++j)
+      *reinterpret_cast<uint2*>(rows + (16 * c + l16) * 256 + ((2 * j + (q4 >> 1)) ^ l16) * 16 + (q4 & 1) * 8) =
+          make_uint2(pack_bf16x2(o[c][j][0] * inv, o[c][j][1] * inv), pack_bf16x2(o[c][j][2] * inv, o[c][j][3] * inv));
+  }
+#pragma unroll
+  for (int i = 0; i < 4 * QT; ++i) {
+    const int r = 4 * i + q4, qry = 16 * QT * w + r;
+    const u32x4 x = *reinterpret_cast<const u32x4*>(rows + r * 256 + (l16 ^ (r & 15)) * 16);
+    if (qry < nq) *reinterpret_cast<u32x4*>(a.o + ((int64_t)(E.row0 + q0 + qry) * a.heads + h) * DH + 8 * l16) = x;
   }
 }
 
