@@ -79,13 +79,14 @@ Kv4Plan kv4_plan(const Rows& rows, int32_t E, int32_t heads, int32_t kv_heads, i
   const int64_t g = heads / kv_heads;
   int64_t small = 0, large = 0;
   for (int32_t e = 0; e < E; ++e) small += ceil_div(rows.count(e) * g, 16), large += ceil_div(rows.count(e) * g, kKv4ChunkRows);
-  P.block_rows = small <= 7 * large ? 16 : kKv4ChunkRows;
-  P.units = (P.block_rows == 16 ? small : large) * kv_heads;
   const int64_t pages = std::max<int64_t>(1, ceil_div(max_length, kKv4Page));
   // Blocks of 16 rows read a page once each, through the L2, where those of 128 read it once; but a block of 128 takes as
   // long as six to eight of 16. By 16 / by 128 in us, 32 heads over 8: 8 sequences of 65536 tokens, 5 rows 148 / 217,
   // 24 rows 318 / 318, 56 rows 690 / 610, 128 rows 1414 / 1209; 16 of 4096, 56 rows 89 / 99, 256 rows 386 / 286; 15 of 4000
-  // with one row and one of 2000 with 512 55 / 65.
+  // with one row and one of 2000 with 512 55 / 65. Where blocks of 128 leave most of the chip without a page, those of 16 are
+  // faster in any case: 32 rows over 16384 tokens 25 / 36, 8 x 32 over 2048 28 / 37, 8 x 64 over 2048 49 / 46.
+  P.block_rows = small <= 7 * large || pages * large * kv_heads <= 1024 ? 16 : kKv4ChunkRows;
+  P.units = (P.block_rows == 16 ? small : large) * kv_heads;
   // Workgroups of 16 rows take four pages at a time, one a wave: eight at least, so that each has one on its way and up to
   // eight pages need no join, but four where that makes at most one workgroup a CU and 32 splits to join. Eight / four, in us:
   // one row of 32 heads over 8, 1024 tokens 8.0 / 9.0, 4096 10.8 / 9.1, 16384 11.3 / 10.3, 32768 14.4 / 16.2; 4 rows over 4096

@@ -804,8 +804,8 @@ hipError_t launch_attn(int kernel, const AttnArgs& a, const AttnBatch& b, hipStr
   if (kernel == 0)
     return wide ? launch_blocks(attn_fwd_stats_kernel<2>, limits[0], 128, a.heads, lds, a, b, K_ATTN_FWD, s)
                 : launch_blocks(attn_fwd_stats_kernel<1>, limits[1], 64, a.heads, lds, a, b, K_ATTN_FWD, s);
-  // Two walks, where the backward is given the forward's output, for few long walks: dQ with one / two, us: 512 workgroups of
-  // up to 32 blocks (2048 rows x 16 heads) 68 / 53, of 64 (4096 x 8) 121 / 91, 256 of 8 (512 x 32) 22 / 18, but of 2 (16 x 128
+  // Two walks, where the backward is given the forward's output (the other keeps its bits), for few long ones. One / two, us:
+  // 512 workgroups of up to 32 blocks (2048 rows x 16 heads) 68 / 53, of 64 (4096 x 8) 121 / 91, 256 of 8 (512 x 32) 22 / 18, but of 2 (16 x 128
   // x 16) 14 / 19; 384 of 8 (6 x 512 x 8) 26 / 26; 1024 of 32 (2048 x 32) 90 / 97; 832 of 104 (6636 x 8) 206 / 223.
   if (a.o && (int64_t)n1 * a.heads <= 512 && longest > 4)
     return launch_blocks(attn_dq_kernel<1, 2>, limits[7], 64, a.heads, 2 * lds, a, b, K_ATTN_DQ, s, 512);

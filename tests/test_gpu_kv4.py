@@ -209,7 +209,8 @@ def test_long_sequences_split(attt, rows, H, kv):
 
 
 @pytest.mark.parametrize("lengths,rows,H,kv", [([2500, 0, 64, 1333, 640, 70], [64] * 6, 4, 1), ([700, 130, 125], [125] * 3, 4, 2),
-                                               ([1500, 1, 0, 900, 1400], [1, 1, 1, 100, 1], 8, 2), ([2000, 90], [9, 9], 10, 1)])
+                                               ([1500, 1, 0, 900, 1400], [1, 1, 1, 100, 1], 8, 2), ([2000, 90], [9, 9], 10, 1),
+                                               ([9000, 300, 128], [32, 32, 32], 32, 8), ([260, 256], [128, 256], 8, 8)])
 def test_row_blocks_beside_each_other(attt, lengths, rows, H, kv):
     """Many query rows of a head's group: whole chunks, chunks beside single tokens, and few rows past a block."""
     s = make(lengths, rows, H, kv, 70 + sum(rows))
@@ -218,6 +219,53 @@ def test_row_blocks_beside_each_other(attt, lengths, rows, H, kv):
     want, _, _ = expected(s)
     assert np.array_equal(cache, want)
     check_attention(s, want, o, lse)
+
+
+def widened(s, width=300):
+    """The same with room for long sequences: the split is by what the host knows, here that they may be long."""
+    return dict(s, table=np.pad(s["table"], ((0, 0), (0, width - s["table"].shape[1])), constant_values=-1))
+
+
+@pytest.mark.parametrize("lengths,rows,H,kv", [([700], [128], 4, 4), ([400, 128, 90, 0], [128] * 4, 4, 4), ([1300, 640], [256, 250], 4, 4),
+                                               ([300, 500], [64, 120], 8, 4), ([2000], [128], 5, 5)])
+def test_full_blocks_of_rows(attt, lengths, rows, H, kv):
+    """Blocks of 128 rows that are nearly full, over sequences that may be long."""
+    s = widened(make(lengths, rows, H, kv, 120 + sum(rows)))
+    note(f"kv4 full blocks: lengths {lengths}, new rows {rows}, {H} heads over {kv}")
+    cache, kh, vh, o, lse = run(attt, s)
+    want, wk, wv = expected(s)
+    assert np.array_equal(cache, want) and np.array_equal(kh, wk) and np.array_equal(vh, wv)
+    check_attention(s, want, o, lse)
+    _, _, _, o2, l2 = run(attt, s)
+    assert np.array_equal(o, o2) and np.array_equal(lse, l2)  # bitwise repeatable
+
+
+def test_full_blocks_with_bad_values(attt):
+    """Lengths and pages that the host cannot check, and infinities in later tokens, where rows fill blocks of 128."""
+    s = widened(make([400, 300, 500], [128] * 3, 4, 4, 131))
+    _, _, _, o0, l0 = run(attt, s)
+    for what in ("page", "length", "negative"):
+        b = dict(s, table=s["table"].copy(), lengths=s["lengths"].copy())
+        if what == "page":
+            b["table"][1, 1] = len(s["cache"])
+        else:
+            b["lengths"][1] = 300 * 128 + 1 if what == "length" else -5
+        note(f"kv4 full blocks: a bad {what}")
+        _, kh, _, o, lse = run(attt, b)
+        keep = np.r_[0:128, 256:384]
+        assert np.array_equal(o[keep], o0[keep]) and np.array_equal(lse[:, keep], l0[:, keep])
+        if what == "negative":
+            assert not o[128:256].any() and np.isneginf(lse[:, 128:256]).all()
+        else:
+            assert np.isnan(o[128:256]).all() and np.isnan(lse[:, 128:256]).all()
+    for name in "kv":  # of row 200, token 300 - 128 + 72 of its sequence
+        b = dict(s, **{name: s[name].copy()})
+        b[name][200, 1, 7] = np.inf
+        _, _, _, o, lse = run(attt, b)
+        seen = np.arange(200, 256)
+        rest = np.setdiff1d(np.arange(384), seen)
+        assert np.array_equal(o[rest], o0[rest]) and np.array_equal(lse[:, rest], l0[:, rest])
+        assert np.array_equal(o[:, [0, 2, 3]], o0[:, [0, 2, 3]]) and np.isnan(o[seen, 1]).all()
 
 
 @pytest.mark.parametrize("lengths,rows,H,kv", [([20000, 0, 130, 9000], [1, 1, 1, 2], 4, 1), ([12345], [1], 2, 2), ([9000, 100], [3, 3], 4, 4)])
