@@ -290,3 +290,23 @@ def test_streams_graphs_and_repeats(attt):
         graph.replay()
         torch.cuda.synchronize()
         assert all(a.equal(b) for a, b in zip((*out, *gout), want)), n
+
+
+@pytest.mark.parametrize("H,kv,N", [(4, 1, 900), (16, 8, 3000), (32, 8, 2048)])
+def test_captured_long_walks(attt, H, kv, N):
+    """Captured, then replayed with eager work between: every replay as the eager calls, for each way of the walks."""
+    import torch
+    q, k, v, do = (dev_dense(x) for x in inputs(N, H, kv, 61 + H))
+    step = lambda: (lambda o: (*o, *attt.attention_bwd_saved(q, k, v, *o, do)))(attt.attention_fwd(q, k, v))  # noqa: E731
+    step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for n in range(3):
+        q.copy_(torch.roll(q, 1, 0))
+        v.mul_(-1.0)
+        want = step()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(a.equal(b) for a, b in zip(got, want)), n

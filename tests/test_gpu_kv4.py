@@ -362,6 +362,30 @@ def test_captured_steps_follow_lengths(attt):
         assert torch.equal(d["cache"], other) and out[0].equal(want[0]) and out[1].equal(want[1]), n
 
 
+@pytest.mark.parametrize("lengths,rows,H,kv", [([700, 300], [128, 128], 4, 4), ([20000], [1], 4, 1), ([600, 90], [40, 3], 8, 2)])
+def test_captured_chunks(attt, lengths, rows, H, kv):
+    """Full blocks of rows, many splits of few rows, several blocks of 16: captured and replayed as the eager calls."""
+    import torch
+    s = widened(make(lengths, rows, H, kv, 140 + sum(rows)))
+    d, other = dev(s), dev(s)["cache"]
+    step = lambda c: (attt.kv4_append(c, d["k"], d["v"], d["table"], d["lengths"], row_offsets=s["off"], want_held=True),  # noqa: E731
+                      attt.kv4_attention(d["q"], c, d["table"], d["lengths"], row_offsets=s["off"]))
+    step(other)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(d["cache"])
+    for n in range(3):
+        d["k"].copy_(torch.roll(d["k"], 1, 0))
+        d["q"].mul_(-0.5)
+        if n == 2:
+            d["lengths"] -= 1
+        want = step(other)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(a.equal(b) for x, y in zip(got, want) for a, b in zip(x, y)) and d["cache"].equal(other), n
+
+
 def test_many_equal_sequences(attt):
     """Decoding batches around a launch's 64 sequences, and chunks of equal rows: the sequence is found by division."""
     for E, rows, H, kv in ((1, 1, 8, 8), (63, 1, 4, 2), (64, 1, 2, 2), (65, 2, 4, 1), (5, 20, 4, 2), (3, 33, 4, 2)):
