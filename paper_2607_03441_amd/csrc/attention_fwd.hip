@@ -271,7 +271,8 @@ __global__ __launch_bounds__(256 * WALKS, 2 / WALKS) void attn_fwd_kernel(AttnAr
       for (int j = 0; j < 8; ++j) o[c][j] = o[c][j] * fa + ex[w][c][j][lane] * fb;
     }
   }
-  // O goes through LDS, chunk c of row r at place c ^ (r % 16), so that whole rows are stored: by a place of its own for each
+  // O goes through LDS, chunk c of row r at place c ^ (r % 16), so that whole rows are stored (32 bytes of a row at a time:
+  // 78 us instead of 73 for 16 ragged prompts of 7001 rows): by a place of its own for each
   // wave, in a buffer that nobody reads any more.
   uint8_t* rows = smem + (WALKS > 1 ? 3 : (kb_last + 1) & 1) * kFwdBuf + w * (16 * QT * DH * 2);
   static_assert(4 * 16 * QT * DH * 2 <= kFwdBuf && (WALKS == 1 || 4 * QT * (8 * 64 * 16 + 64 * 8) <= 3 * kFwdBuf), "LDS");
@@ -328,11 +329,11 @@ static hipError_t launch_fwd(LdsLimit& limit, const AttnArgs& a, AttnBatch b, hi
 
 // One or two query tiles a wave and one or two walks, by an estimate in microseconds of the launch: starts and ends of the
 // workgroups and their steps of 64 keys, spread over the CUs, against the longest walk; the larger of the two and a part of the
-// other. Fitted to 55 shapes of 64 to 30000 rows (rms errors 7 to 8%), over which the choice takes 1.008 times the
-// best one's time on average (without two walks 1.097). One tile / two / one and two walks / two and two walks: 100
-// rows x 16 heads 5.9 / 8.6 / 6.3 / 8.6; 4096 x 4 56 / 78 / 42.5 / 60; 2048 x 16 36.0 / 44.5 / 32.2 / 36.2; 8192 x 8
-// 172 / 175 / 179 / 140; 8192 x 32 637 / 508 / 690 / 530; 16 x 128 x 32 15.6 / 14.7 / 25.1 / 20.1. Farthest from the
-// best: 2 x 1000 x 32 takes 38 with the chosen two tiles, 32 with one.
+// other. Fitted to 55 shapes of 64 to 30000 rows (rms errors 7 to 8%), over which the choice takes 1.012 times the
+// best one's time on average (without two walks 1.101). One tile / two / one and two walks / two and two walks: 100
+// rows x 16 heads 5.6 / 7.7 / 6.0 / 8.2; 4096 x 4 53 / 77 / 40.2 / 58; 2048 x 16 33.5 / 43.7 / 29.5 / 35.1; 8192 x 8
+// 170 / 171 / 175 / 137; 8192 x 32 621 / 496 / 678 / 526; 16 x 128 x 32 14.7 / 13.3 / 23.0 / 18.9. Farthest from the
+// best: 2 x 1000 x 32 takes 37 with the chosen two tiles, 31 with one.
 hipError_t launch_attn_fwd(const AttnArgs& a, const AttnBatch& b, hipStream_t s) {
   static LdsLimit limits[4];
   double wgs[2] = {}, steps[2] = {}, longest = 0.0;
