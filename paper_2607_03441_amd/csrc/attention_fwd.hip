@@ -287,6 +287,10 @@ __global__ __launch_bounds__(256 * WALKS, 2 / WALKS) void attn_fwd_kernel(AttnAr
       *reinterpret_cast<uint2*>(rows + (16 * c + l16) * 256 + ((2 * j + (q4 >> 1)) ^ l16) * 16 + (q4 & 1) * 8) =
           make_uint2(pack_bf16x2(o[c][j][0] * inv, o[c][j][1] * inv), pack_bf16x2(o[c][j][2] * inv, o[c][j][3] * inv));
   }
+  // the wave's own writes come before its reads; no other wave takes part
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 #pragma unroll
   for (int i = 0; i < 4 * QT; ++i) {
     const int r = 4 * i + q4, qry = 16 * QT * w + r;
